@@ -53,6 +53,7 @@ enum {
 
 typedef enum { LPDT_SYM_S8 = 0, LPDT_AFFINE_U8 = 1 } lpdt_qmode;
 typedef enum { LPDT_ROUND_NEAREST_EVEN = 0, LPDT_ROUND_STOCHASTIC = 1 } lpdt_round;
+typedef enum { LPDT_F32 = 0, LPDT_BF16 = 1, LPDT_F16 = 2 } lpdt_dtype;
 
 /* Convolution geometry.  Ho = (H + 2*pad - R)/stride + 1, likewise Wo.
  * A linear layer is R = S = H = W = 1, stride 1, pad 0 (B rows, Cin -> Cout). */
@@ -281,6 +282,51 @@ lpdt_status lpdt_qconv_bwd_weight_affine(const lpdt_conv_desc *d, const uint8_t 
                                          const uint8_t *A, const float *sA, const int32_t *zA,
                                          float *dW, int64_t dw_node_stride, int32_t *dWacc,
                                          void *ws, size_t ws_bytes, int32_t *dev_status, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * 8-bit floats with a scale for each block of 128 values.
+ * (The paper quantizes to 8-bit integers with one range per tensor; this is the finer format beside it, for layers
+ * whose values spread too far for one range.)
+ *
+ * A matrix [nodes][rows][cols] is held as e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; largest value 448, 0x7f NaN)
+ * and one scale byte s per row and 128 consecutive columns, which stands for 2^(s-127) (255: NaN):
+ *   value[r][c] = code[r][c] * 2^(scale[r][c/128] - 127)
+ *   codes   [nodes][rows][lpdt_e4m3_pitch(cols)]         (cols rounded up to 16), 16-byte aligned
+ *   scales  [nodes][rows][lpdt_e4m3_scale_pitch(cols)]   (ceil(cols/128) rounded up to 4), 4-byte aligned
+ * What lies in a row behind its last column, or last block, is never used.  Both return -1 for cols < 0.
+ *
+ * lpdt_quantize_e4m3 - codes and scales of x, in one pass over it.
+ *   e = the least integer >= -127 with amax <= 448 * 2^e, amax = max|x| of the block (amax = 0: e = 0);
+ *   scale = e + 127;  code = x * 2^-e rounded to nearest, halves to even (the product is exact).
+ *   A block that holds a NaN or an infinity reads as NaN throughout (scale 255, codes 0x7f).
+ * x        : `dtype` elements, x[n][r][c] at n*x_node_stride + r*x_row_stride + c (elements)
+ * q, scale : the matrix itself, blocks along its rows;  qt, scale_t : its transpose [nodes][cols][rows], blocks along
+ *            x's columns.  Either pair may be NULL, not both.  A contraction over columns takes the first form, one over
+ *            rows the second, so the three products of a linear layer Y = X W^T are lpdt_matmul_e4m3 of
+ *            (X, W), (dY, W transposed) and (dY transposed, X transposed).
+ * scale and scale_t need no alignment here.  Codes are written up to their pitch (zeros behind the last column).
+ * Errors: INVALID_ARG, UNSUPPORTED (a dimension above 2^30, 2^31 blocks or more), CUDA.  Empty matrices are a no-op.
+ */
+int64_t lpdt_e4m3_pitch(int64_t cols);
+int64_t lpdt_e4m3_scale_pitch(int64_t cols);
+lpdt_status lpdt_quantize_e4m3(const void *x, lpdt_dtype dtype, int32_t nodes, int64_t rows, int64_t cols,
+                               int64_t x_node_stride, int64_t x_row_stride, uint8_t *q, uint8_t *scale,
+                               uint8_t *qt, uint8_t *scale_t, void *stream);
+
+/* lpdt_matmul_e4m3 - product of two such matrices, contracted over their columns:
+ *   C[n][m][j] = sum_k A[n][m][k] * B[n][j][k]  (+ bias[n][j])  (+ addend[n][m][j])
+ * A [nodes][M][K], B [nodes][N][K] with their scales sA, sB as above;  fp32 accumulation over all of K, each of the two
+ * additions one more fp32 rounding, then one rounding to the type of C.
+ * C      : `c_dtype`, C[n][m][j] at n*c_node_stride + m*c_row_stride + j (so it may be a tensor inside a flat gradient
+ *          vector);  nothing between the rows is written
+ * bias   : fp32, node n at bias + n*bias_node_stride, N entries (nullable)
+ * addend : type and strides of C (nullable); may be C itself, which accumulates
+ * K >= 1; M, N or nodes = 0 is a no-op.  dev_status (nullable): LPDT_ERR_TIMEOUT from a bounded wait that ran out.
+ * Errors: INVALID_ARG, UNSUPPORTED (a dimension above 2^30), CUDA. */
+lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int64_t K, const uint8_t *A, const uint8_t *sA,
+                             const uint8_t *B, const uint8_t *sB, const float *bias, int64_t bias_node_stride,
+                             const void *addend, void *C, lpdt_dtype c_dtype, int64_t c_node_stride,
+                             int64_t c_row_stride, int32_t *dev_status, void *stream);
 
 /* ---------------------------------------------------------------------------
  * Range-EvoNorm (Eq. "ren"), forward and backward.

@@ -16,7 +16,7 @@ from ._lib import lib as _load
 
 
 # Entry points that enqueue kernels (wrapped for the optional call log and per-call timing).
-LAUNCHING = {"lpdt_quantize", "lpdt_quantize_with_range", "lpdt_quantize_static", "lpdt_quantize_batch", "lpdt_dequantize", "lpdt_qconv_fwd", "lpdt_qconv_fwd_affine", "lpdt_qconv_bwd_data_affine", "lpdt_qconv_bwd_weight_affine", "lpdt_qconv_bwd_data", "lpdt_qconv_bwd_weight", "lpdt_range_evonorm_fwd", "lpdt_range_evonorm_bwd", "lpdt_range_evonorm_fwd_q8", "lpdt_range_evonorm_bwd_q8", "lpdt_range_evonorm_pool_fwd", "lpdt_range_evonorm_pool_bwd", "lpdt_range_evonorm_bwd_params", "lpdt_range_evonorm_bwd_params_batch", "lpdt_dequantize_acc_batch", "lpdt_gossip_mix", "lpdt_gossip_mix_q8", "lpdt_deepsqueeze_mix", "lpdt_pushsum_debias", "lpdt_sgd_gossip_mix", "lpdt_evonorm_s0_fwd", "lpdt_evonorm_s0_bwd", "lpdt_range_bn_fwd", "lpdt_range_bn_bwd", "lpdt_sgd_update", "lpdt_residual_add", "lpdt_residual_add_bwd", "lpdt_avgpool", "lpdt_avgpool_bwd", "lpdt_maxpool2x2", "lpdt_maxpool2x2_bwd", "lpdt_softmax_ce", "lpdt_colsum", "lpdt_selftest_bounded_wait"}
+LAUNCHING = {"lpdt_quantize", "lpdt_quantize_with_range", "lpdt_quantize_static", "lpdt_quantize_batch", "lpdt_dequantize", "lpdt_qconv_fwd", "lpdt_qconv_fwd_affine", "lpdt_qconv_bwd_data_affine", "lpdt_qconv_bwd_weight_affine", "lpdt_qconv_bwd_data", "lpdt_qconv_bwd_weight", "lpdt_range_evonorm_fwd", "lpdt_range_evonorm_bwd", "lpdt_range_evonorm_fwd_q8", "lpdt_range_evonorm_bwd_q8", "lpdt_range_evonorm_pool_fwd", "lpdt_range_evonorm_pool_bwd", "lpdt_range_evonorm_bwd_params", "lpdt_range_evonorm_bwd_params_batch", "lpdt_dequantize_acc_batch", "lpdt_gossip_mix", "lpdt_gossip_mix_q8", "lpdt_deepsqueeze_mix", "lpdt_pushsum_debias", "lpdt_sgd_gossip_mix", "lpdt_evonorm_s0_fwd", "lpdt_evonorm_s0_bwd", "lpdt_range_bn_fwd", "lpdt_range_bn_bwd", "lpdt_sgd_update", "lpdt_residual_add", "lpdt_residual_add_bwd", "lpdt_avgpool", "lpdt_avgpool_bwd", "lpdt_maxpool2x2", "lpdt_maxpool2x2_bwd", "lpdt_softmax_ce", "lpdt_colsum", "lpdt_selftest_bounded_wait", "lpdt_quantize_e4m3", "lpdt_matmul_e4m3"}
 # A thread that records (see Calls) gets a library whose launching entry points note their arguments as they run.
 class _Recording(threading.local):
     calls = None
@@ -256,6 +256,42 @@ def lpdt_qconv_bwd_weight(desc, E, sE, A, sA, dW=None, dw_node_stride=0, dWacc=N
 
 def lpdt_qconv_bwd_weight_direct(desc):
     return lib().lpdt_qconv_bwd_weight_direct(C.byref(desc))
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}          # lpdt_dtype
+
+
+def _dtype(t):
+    assert t.dtype in DTYPES, f"fp32, bf16 or fp16 tensor expected, not {t.dtype}"
+    return DTYPES[t.dtype]
+
+
+def lpdt_e4m3_pitch(cols):
+    return lib().lpdt_e4m3_pitch(cols)
+
+
+def lpdt_e4m3_scale_pitch(cols):
+    return lib().lpdt_e4m3_scale_pitch(cols)
+
+
+def lpdt_quantize_e4m3(x, nodes, rows, cols, q=None, scale=None, qt=None, scale_t=None, x_row_stride=None,
+                       x_node_stride=None):
+    """x fp32, bf16 or fp16; q, scale: blocks of 128 along the rows; qt, scale_t: of the transpose."""
+    xr = cols if x_row_stride is None else x_row_stride
+    xn = rows * xr if x_node_stride is None else x_node_stride
+    _check("lpdt_quantize_e4m3", lib().lpdt_quantize_e4m3(_ptr(x), _dtype(x), nodes, rows, cols, xn, xr, _ptr(q), _ptr(scale),
+                                                          _ptr(qt), _ptr(scale_t), _stream()))
+
+
+def lpdt_matmul_e4m3(nodes, M, N, K, A, sA, B, sB, C, bias=None, bias_node_stride=0, addend=None, c_row_stride=None,
+                     c_node_stride=None, dev_status=None):
+    """C = A B^T (+ bias) (+ addend) of two matrices as lpdt_quantize_e4m3 writes them; addend of C's type and strides."""
+    cr = N if c_row_stride is None else c_row_stride
+    cn = M * cr if c_node_stride is None else c_node_stride
+    assert addend is None or addend.dtype == C.dtype, "addend has the type of C"
+    _check("lpdt_matmul_e4m3", lib().lpdt_matmul_e4m3(
+        nodes, M, N, K, _ptr(A), _ptr(sA), _ptr(B), _ptr(sB), _ptr(bias), bias_node_stride, _ptr(addend), _ptr(C), _dtype(C),
+        cn, cr, _ptr(dev_status), _stream()))
 
 
 def lpdt_range_evonorm_fwd(nodes, B, H, W, Cc, groups, eps, x, v, gamma, beta, param_node_stride, y,

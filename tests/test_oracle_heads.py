@@ -1,0 +1,79 @@
+"""Pins of the oracle of the output head's operators, and the refusals of their entry points (checked on the host, so no
+GPU is needed: nothing is enqueued)."""
+import numpy as np
+import pytest
+
+from oracle import heads
+from paper_2111_09389_b200 import _lib
+
+OK, INVALID, UNSUPPORTED = 0, 1, 2
+P = 1 << 20          # a device address that no call gets as far as using
+
+
+# ------------------------------------------------------------------ 8-bit floats
+def test_codes_and_their_values():
+    """Values of the format by hand, every code's own value, halves to the even code, halves beyond the last step."""
+    hand = {0x00: 0.0, 0x01: 2.0 ** -9, 0x07: 7 * 2.0 ** -9, 0x08: 2.0 ** -6, 0x38: 1.0, 0x39: 1.125, 0x7e: 448.0, 0xb8: -1.0, 0xfe: -448.0}
+    for code, value in hand.items():
+        assert heads.E4M3[code] == value
+        assert heads.e4m3_encode(np.array([value]))[0] == code
+    codes = np.array([c for c in range(256) if c not in (0x7f, 0xff)])
+    assert np.array_equal(heads.e4m3_encode(heads.E4M3[codes]), codes)
+    mid = (heads.E4M3[0x38] + heads.E4M3[0x39]) / 2, (heads.E4M3[0x39] + heads.E4M3[0x3a]) / 2
+    assert list(heads.e4m3_encode(np.array(mid))) == [0x38, 0x3a]
+    assert list(heads.e4m3_encode(np.array([2.0 ** -10, 1.5 * 2.0 ** -9, -2.0 ** -11]))) == [0x00, 0x02, 0x80]
+
+
+def test_scales_at_their_borders():
+    x = np.zeros((6, 130))
+    x[0, 0], x[1, 0], x[2, 0], x[3, 0], x[4, 0] = 448, np.nextafter(448, 500), 2.0 ** -149, np.inf, 1.0
+    x[4, 129] = -7.0
+    q, s = heads.quantize_e4m3(x)
+    assert [list(r) for r in s] == [[127, 127], [128, 127], [0, 127], [255, 127], [119, 121], [127, 127]]
+    assert q[0, 0] == 0x7e and q[1, 0] == 0x76 and (q[3, :128] == 0x7f).all() and q[3, 128] == 0
+    assert heads.E4M3[q[4, 0]] * 2.0 ** -8 == 1.0 and heads.E4M3[q[4, 129]] * 2.0 ** -6 == -7.0
+    v = heads.dequantize_e4m3(q, s)
+    assert v[4, 129] == -7.0 and np.isnan(v[3, :128]).all() and v[3, 129] == 0
+
+
+def test_product_by_hand():
+    q, s = heads.quantize_e4m3(np.array([[[1.0, -2.0, 0.5]], [[4.0, 0.0, 1.0]]]))
+    r, t = heads.quantize_e4m3(np.array([[[3.0, 1.0, 2.0], [0.0, 0.0, 0.25]], [[1.0, 5.0, 8.0], [2.0, 2.0, 2.0]]]))
+    c, size = heads.matmul_e4m3(q, s, r, t, bias=np.array([[1.0, 0.0], [0.0, -1.0]]))
+    assert c.tolist() == [[[3.0, 0.125]], [[12.0, 9.0]]] and size.tolist() == [[[6.0, 0.125]], [[12.0, 10.0]]]
+
+
+def test_pitches():
+    L = _lib.lib()
+    assert [L.lpdt_e4m3_pitch(c) for c in (0, 1, 16, 17, 1000)] == [0, 16, 16, 32, 1008]
+    assert [L.lpdt_e4m3_scale_pitch(c) for c in (0, 1, 128, 129, 512, 513, 4096)] == [0, 4, 4, 4, 4, 8, 32]
+    assert L.lpdt_e4m3_pitch(-1) == -1 and L.lpdt_e4m3_scale_pitch(-1) == -1
+
+
+def test_quantizer_refusals():
+    names = "x dtype nodes rows cols x_node x_row q scale qt scale_t stream".split()
+    base = dict(x=P, dtype=0, nodes=2, rows=3, cols=5, x_node=15, x_row=5, q=P, scale=P, qt=P, scale_t=P, stream=0)
+    call = lambda **kw: _lib.lib().lpdt_quantize_e4m3(*[{**base, **kw}[n] for n in names])
+    for empty in (dict(nodes=0), dict(rows=0), dict(cols=0), dict(nodes=0, x=0, q=0, scale=0)):
+        assert call(**empty) == OK
+    for bad in (dict(x=0), dict(dtype=3), dict(dtype=-1), dict(nodes=-1), dict(rows=-1), dict(cols=-1), dict(scale=0), dict(q=0),
+                dict(qt=0), dict(scale_t=0), dict(q=0, scale=0, qt=0, scale_t=0), dict(x_row=4), dict(x_node=-1), dict(q=P + 8),
+                dict(qt=P + 1), dict(x=P + 2), dict(x=P + 1, dtype=1)):
+        assert call(**bad) == INVALID, bad
+    assert call(rows=1 << 31, qt=0, scale_t=0) == UNSUPPORTED
+    assert call(rows=1 << 30, cols=512, x_row=512, qt=0, scale_t=0) == UNSUPPORTED
+    assert call(rows=1 << 24) == UNSUPPORTED
+
+
+def test_product_refusals():
+    names = "nodes M N K A sA B sB bias bias_node addend C c_dtype c_node c_row status stream".split()
+    base = dict(nodes=2, M=3, N=5, K=7, A=P, sA=P, B=P, sB=P, bias=0, bias_node=0, addend=0, C=P, c_dtype=0, c_node=15, c_row=5,
+                status=0, stream=0)
+    call = lambda **kw: _lib.lib().lpdt_matmul_e4m3(*[{**base, **kw}[n] for n in names])
+    for empty in (dict(nodes=0), dict(M=0), dict(N=0), dict(N=0, A=0, C=0)):
+        assert call(**empty) == OK
+    for bad in (dict(nodes=-1), dict(M=-1), dict(N=-1), dict(K=0), dict(K=-5), dict(A=0), dict(sA=0), dict(B=0), dict(sB=0), dict(C=0),
+                dict(c_dtype=7), dict(A=P + 8), dict(B=P + 4), dict(sA=P + 2), dict(sB=P + 1), dict(C=P + 2), dict(addend=P + 1),
+                dict(c_row=4), dict(c_node=14), dict(bias=P, bias_node=-1), dict(bias=P + 2)):
+        assert call(**bad) == INVALID, bad
+    assert call(K=(1 << 30) + 1) == UNSUPPORTED and call(M=1 << 31, c_node=1 << 40) == UNSUPPORTED
