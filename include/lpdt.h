@@ -632,6 +632,60 @@ lpdt_status lpdt_softmax_ce(int32_t nodes, int32_t B, int32_t K, const float *lo
                             const int32_t *labels, float *loss, float *dlogits, int32_t *dev_status,
                             void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Reports and losses on rows of logits, beside lpdt_softmax_ce (no counterpart in the paper): what a node says about its
+ * own predictions, and what another node learns from it.  A node that sends the top k log probabilities of a row sends
+ * k values and k positions, as a compressed update does in lpdt_gossip_mix.
+ *
+ * logits : `dtype` (fp32, bf16 or fp16), row r at r*row_stride, V of them;  z = logits / temperature (1e-30 to 1e30).
+ * Sums are held in fp32 relative to the row's running maximum and joined with the rest in double.  -inf marks a token that
+ * has no probability.  A row that holds a NaN or +inf answers NaN.  Rows may start at any element (16-byte accesses inside).
+ *
+ * lpdt_token_logprobs
+ *   lse[r] = ln sum_v e^z;  logprob[r] = z[tokens[r]] - lse[r];  entropy[r] = -sum_v p ln p, p = e^(z - lse) (0 ln 0 = 0)
+ *   top_logprob, top_index [rows][top_k]: the top_k largest, largest first, of equal logits the lower position first
+ * A row of nothing but -inf: logprob = lse = -inf, entropy 0.  tokens[r] < 0: no token, logprob 0.  tokens[r] >= V:
+ * the same, and LPDT_ERR_INVALID_ARG in dev_status (one int32, caller-zeroed, nullable).  NaN is never among the top_k;
+ * where nothing else is left the index is -1.
+ * tokens : int32 [rows], needed for logprob only.  logprob, entropy, lse : fp32 [rows], each nullable;  top_k 0 to 128.
+ * Errors: INVALID_ARG (top_k > V included), UNSUPPORTED (top_k > 128, V > 2^30, rows > 2^27), CUDA.
+ *
+ * lpdt_token_logprobs_bwd - from lse and entropy as the forward wrote them,
+ *   dlogits[r][v] = (1[v = tokens[r]] * g - p * (g + h * (ln p + entropy) - l)) / temperature
+ * with g = d_logprob[r] (0 where the row has no token), h = d_entropy[r], l = d_lse[r]; each of the three nullable, not
+ * all.  tokens is needed with d_logprob, entropy with d_entropy.  p is taken from the fp32 lse, so it is off by up to
+ * 2^-23 * |lse| relative.  A row of nothing but mask values (lse < -1e30) has no gradient.  dlogits : `dtype`; it may be
+ * the logits themselves with the same stride. */
+lpdt_status lpdt_token_logprobs(int64_t rows, int32_t V, const void *logits, lpdt_dtype dtype, int64_t row_stride,
+                                float temperature, const int32_t *tokens, float *logprob, float *entropy, float *lse,
+                                int32_t top_k, float *top_logprob, int32_t *top_index, int32_t *dev_status, void *stream);
+lpdt_status lpdt_token_logprobs_bwd(int64_t rows, int32_t V, const void *logits, lpdt_dtype dtype, int64_t row_stride,
+                                    float temperature, const int32_t *tokens, const float *lse, const float *entropy,
+                                    const float *d_logprob, const float *d_entropy, const float *d_lse, void *dlogits,
+                                    int64_t dlogits_row_stride, void *stream);
+
+/* lpdt_distill_topk - distillation from a teacher's top k log probabilities (taken at the same temperature), as
+ * lpdt_token_logprobs writes them: the Kullback-Leibler divergence from the teacher to the student's p, per row
+ *   tail = 1: t_j = e^teacher_logprob[j];  what the list leaves, t_R = max(0, 1 - sum t), is one more class, which the
+ *             student gives p_R = sum of p over the tokens that are not listed:
+ *             L = sum_j t_j (ln t_j - ln p[index j]) + t_R (ln t_R - ln p_R)
+ *   tail = 0: t = softmax of teacher_logprob over the list (so any additive constant is free; a list of nothing but
+ *             -inf has no target: loss and gradient 0), no last term
+ * (0 ln 0 = 0; with nothing outside the list the last term is left out).  With t_v the sum over the entries of token v,
+ *   dL/dlogits[v] = (p[v] (sum t + t_R) - t_v) / temperature                    for listed v
+ *                   (p[v] (sum t + t_R) - t_R p[v] / p_R) / temperature         for the others
+ * row_loss[n][b] = L;  loss[n] = sum_b row_weight L / B;  dlogits = row_weight / B * dL/dlogits, the gradient of the loss.
+ * logits, dlogits (nullable: loss only; may be the logits themselves with the same stride) : rows n*B + b as above.
+ * teacher_logprob fp32, teacher_index int32 : [nodes][B][k], k 1 to 128 (it may exceed V).  An index < 0 is no entry; one
+ * >= V is none either and puts LPDT_ERR_INVALID_ARG into dev_status.  A token may be listed more than once.
+ * row_weight : fp32 [nodes][B] (nullable: 1).  A row of weight 0 is not read: row_loss 0, gradient 0; so is a student's row
+ * of nothing but mask values (lse < -1e30).  loss fp32 [nodes], row_loss fp32 [nodes][B].
+ * Errors: INVALID_ARG, UNSUPPORTED (k > 128, V > 2^20, nodes*B > 2^27), CUDA. */
+lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, const void *logits, lpdt_dtype dtype, int64_t row_stride,
+                              float temperature, int32_t k, const float *teacher_logprob, const int32_t *teacher_index,
+                              int32_t tail, const float *row_weight, float *loss, float *row_loss, void *dlogits,
+                              int64_t dlogits_row_stride, int32_t *dev_status, void *stream);
+
 /* out[n][c] = sum_b x[n][b][c] (bias gradient); node n of out at out + n*out_node_stride. */
 lpdt_status lpdt_colsum(int32_t nodes, int32_t B, int32_t C, const float *x,
                         float *out, int64_t out_node_stride, void *stream);

@@ -74,8 +74,8 @@ def _log_softmax(z):
     m = z.max(-1, keepdims=True)
     m = np.where(m == -np.inf, 0, m)
     with np.errstate(divide="ignore", invalid="ignore"):
-        lse = m + np.log(np.exp(z - m).sum(-1, keepdims=True))
-        return np.where(z == -np.inf, -np.inf, z - lse), lse
+        log_sum = np.log(np.exp(z - m).sum(-1, keepdims=True))
+        return np.where((z == -np.inf) & ~np.isnan(log_sum), -np.inf, (z - m) - log_sum), m + log_sum
 
 
 def token_logprobs(logits, tokens, temperature=1.0, top_k=0):
@@ -109,7 +109,8 @@ def token_logprobs_bwd(logits, tokens, d_logprob=None, d_entropy=None, d_lse=Non
     onehot = np.zeros_like(z)
     np.put_along_axis(onehot, np.where(some, tokens[:, None], 0), some.astype(float), -1)
     g = np.where(some, g, 0)
-    return ((onehot - p) * g - h * (plogp - p * plogp.sum(-1, keepdims=True)) + l * p) / temperature
+    none = z.max(-1, keepdims=True) < -1e30                   # nothing but mask values: no gradient
+    return np.where(none, 0, (onehot - p) * g - h * (plogp - p * plogp.sum(-1, keepdims=True)) + l * p) / temperature
 
 
 def distill_topk(logits, value, index, tail, temperature=1.0, row_weight=None):
@@ -121,7 +122,7 @@ def distill_topk(logits, value, index, tail, temperature=1.0, row_weight=None):
     row_loss, grad = np.zeros((nodes, B)), np.zeros_like(z)
     for n in range(nodes):
         for b in range(B):
-            if w[n, b] == 0:
+            if w[n, b] == 0 or z[n, b].max() < -1e30:         # left out, or nothing but mask values
                 continue
             have = (index[n, b] >= 0) & (index[n, b] < V)
             ids, lt = index[n, b][have], np.asarray(value[n, b], np.float64)[have]
@@ -129,8 +130,8 @@ def distill_topk(logits, value, index, tail, temperature=1.0, row_weight=None):
             logp = logp[0]
             with np.errstate(divide="ignore", invalid="ignore"):
                 p = np.exp(logp)
-                if not tail:
-                    lt = lt - lt.max() - np.log(np.exp(lt - lt.max()).sum()) if len(lt) else lt
+                if not tail and len(lt) and lt.max() > -np.inf:       # a list without any mass stays without
+                    lt = lt - lt.max() - np.log(np.exp(lt - lt.max()).sum())
                 t = np.exp(lt)
                 live = t > 0
                 loss = (t[live] * (lt[live] - logp[ids[live]])).sum()

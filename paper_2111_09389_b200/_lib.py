@@ -86,6 +86,9 @@ SIGNATURES = {
     "lpdt_maxpool2x2": (_i32, [_i32] * 5 + [_vp] * 4),
     "lpdt_maxpool2x2_bwd": (_i32, [_i32] * 5 + [_vp] * 4),
     "lpdt_softmax_ce": (_i32, [_i32] * 3 + [_vp] * 6),
+    "lpdt_token_logprobs": (_i32, [_i64, _i32, _vp, _i32, _i64, _f32] + [_vp] * 4 + [_i32] + [_vp] * 4),
+    "lpdt_token_logprobs_bwd": (_i32, [_i64, _i32, _vp, _i32, _i64, _f32] + [_vp] * 7 + [_i64, _vp]),
+    "lpdt_distill_topk": (_i32, [_i32] * 3 + [_vp, _i32, _i64, _f32, _i32, _vp, _vp, _i32] + [_vp] * 4 + [_i64, _vp, _vp]),
     "lpdt_colsum": (_i32, [_i32] * 3 + [_vp, _vp, _i64, _vp]),
     "lpdt_call_id": (_i32, [C.c_char_p]),
     "lpdt_run_calls": (_i32, [_vp, _i64, _vp, _i32, _vp]),

@@ -16,7 +16,7 @@ from ._lib import lib as _load
 
 
 # Entry points that enqueue kernels (wrapped for the optional call log and per-call timing).
-LAUNCHING = {"lpdt_quantize", "lpdt_quantize_with_range", "lpdt_quantize_static", "lpdt_quantize_batch", "lpdt_dequantize", "lpdt_qconv_fwd", "lpdt_qconv_fwd_affine", "lpdt_qconv_bwd_data_affine", "lpdt_qconv_bwd_weight_affine", "lpdt_qconv_bwd_data", "lpdt_qconv_bwd_weight", "lpdt_range_evonorm_fwd", "lpdt_range_evonorm_bwd", "lpdt_range_evonorm_fwd_q8", "lpdt_range_evonorm_bwd_q8", "lpdt_range_evonorm_pool_fwd", "lpdt_range_evonorm_pool_bwd", "lpdt_range_evonorm_bwd_params", "lpdt_range_evonorm_bwd_params_batch", "lpdt_dequantize_acc_batch", "lpdt_gossip_mix", "lpdt_gossip_mix_q8", "lpdt_deepsqueeze_mix", "lpdt_pushsum_debias", "lpdt_sgd_gossip_mix", "lpdt_evonorm_s0_fwd", "lpdt_evonorm_s0_bwd", "lpdt_range_bn_fwd", "lpdt_range_bn_bwd", "lpdt_sgd_update", "lpdt_residual_add", "lpdt_residual_add_bwd", "lpdt_avgpool", "lpdt_avgpool_bwd", "lpdt_maxpool2x2", "lpdt_maxpool2x2_bwd", "lpdt_softmax_ce", "lpdt_colsum", "lpdt_selftest_bounded_wait", "lpdt_quantize_e4m3", "lpdt_matmul_e4m3"}
+LAUNCHING = {"lpdt_quantize", "lpdt_quantize_with_range", "lpdt_quantize_static", "lpdt_quantize_batch", "lpdt_dequantize", "lpdt_qconv_fwd", "lpdt_qconv_fwd_affine", "lpdt_qconv_bwd_data_affine", "lpdt_qconv_bwd_weight_affine", "lpdt_qconv_bwd_data", "lpdt_qconv_bwd_weight", "lpdt_range_evonorm_fwd", "lpdt_range_evonorm_bwd", "lpdt_range_evonorm_fwd_q8", "lpdt_range_evonorm_bwd_q8", "lpdt_range_evonorm_pool_fwd", "lpdt_range_evonorm_pool_bwd", "lpdt_range_evonorm_bwd_params", "lpdt_range_evonorm_bwd_params_batch", "lpdt_dequantize_acc_batch", "lpdt_gossip_mix", "lpdt_gossip_mix_q8", "lpdt_deepsqueeze_mix", "lpdt_pushsum_debias", "lpdt_sgd_gossip_mix", "lpdt_evonorm_s0_fwd", "lpdt_evonorm_s0_bwd", "lpdt_range_bn_fwd", "lpdt_range_bn_bwd", "lpdt_sgd_update", "lpdt_residual_add", "lpdt_residual_add_bwd", "lpdt_avgpool", "lpdt_avgpool_bwd", "lpdt_maxpool2x2", "lpdt_maxpool2x2_bwd", "lpdt_softmax_ce", "lpdt_colsum", "lpdt_selftest_bounded_wait", "lpdt_quantize_e4m3", "lpdt_matmul_e4m3", "lpdt_token_logprobs", "lpdt_token_logprobs_bwd", "lpdt_distill_topk"}
 # A thread that records (see Calls) gets a library whose launching entry points note their arguments as they run.
 class _Recording(threading.local):
     calls = None
@@ -517,6 +517,34 @@ def lpdt_maxpool2x2_bwd(nodes, B, H, W, Cc, dy, idx, dx):
 def lpdt_softmax_ce(nodes, B, K, logits, labels, loss, dlogits, dev_status=None):
     _check("lpdt_softmax_ce", lib().lpdt_softmax_ce(nodes, B, K, _ptr(logits), _ptr(labels), _ptr(loss),
                                                     _ptr(dlogits), _ptr(dev_status), _stream()))
+
+
+def lpdt_token_logprobs(rows, V, logits, tokens=None, logprob=None, entropy=None, lse=None, top_logprob=None, top_index=None,
+                        top_k=0, temperature=1.0, row_stride=None, dev_status=None):
+    """logits fp32, bf16 or fp16 [rows][V]; tokens, top_index int32; the rest fp32."""
+    _check("lpdt_token_logprobs", lib().lpdt_token_logprobs(
+        rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _ptr(tokens), _ptr(logprob),
+        _ptr(entropy), _ptr(lse), top_k, _ptr(top_logprob), _ptr(top_index), _ptr(dev_status), _stream()))
+
+
+def lpdt_token_logprobs_bwd(rows, V, logits, tokens, lse, entropy, dlogits, d_logprob=None, d_entropy=None, d_lse=None,
+                            temperature=1.0, row_stride=None, dlogits_row_stride=None):
+    """lse, entropy as the forward wrote them; dlogits of the logits' type."""
+    assert dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
+    _check("lpdt_token_logprobs_bwd", lib().lpdt_token_logprobs_bwd(
+        rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _ptr(tokens), _ptr(lse),
+        _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(d_lse), _ptr(dlogits),
+        V if dlogits_row_stride is None else dlogits_row_stride, _stream()))
+
+
+def lpdt_distill_topk(nodes, B, V, logits, k, teacher_logprob, teacher_index, loss, row_loss, dlogits=None, row_weight=None,
+                      tail=True, temperature=1.0, row_stride=None, dlogits_row_stride=None, dev_status=None):
+    """teacher_logprob fp32, teacher_index int32 [nodes][B][k]; dlogits of the logits' type."""
+    assert dlogits is None or dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
+    _check("lpdt_distill_topk", lib().lpdt_distill_topk(
+        nodes, B, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, k, _ptr(teacher_logprob),
+        _ptr(teacher_index), int(tail), _ptr(row_weight), _ptr(loss), _ptr(row_loss), _ptr(dlogits),
+        V if dlogits_row_stride is None else dlogits_row_stride, _ptr(dev_status), _stream()))
 
 
 def lpdt_colsum(nodes, B, Cc, x, out, out_node_stride):

@@ -47,7 +47,8 @@ static const Entry kEntries[] = {
     LPDT_ENTRY(lpdt_gossip_mix), LPDT_ENTRY(lpdt_gossip_mix_q8), LPDT_ENTRY(lpdt_sgd_gossip_mix), LPDT_ENTRY(lpdt_sgd_update),
     LPDT_ENTRY(lpdt_residual_add), LPDT_ENTRY(lpdt_residual_add_bwd), LPDT_ENTRY(lpdt_avgpool), LPDT_ENTRY(lpdt_avgpool_bwd),
     LPDT_ENTRY(lpdt_maxpool2x2), LPDT_ENTRY(lpdt_maxpool2x2_bwd), LPDT_ENTRY(lpdt_softmax_ce), LPDT_ENTRY(lpdt_colsum),
-    LPDT_ENTRY(lpdt_quantize_e4m3), LPDT_ENTRY(lpdt_matmul_e4m3)};
+    LPDT_ENTRY(lpdt_quantize_e4m3), LPDT_ENTRY(lpdt_matmul_e4m3),
+    LPDT_ENTRY(lpdt_token_logprobs), LPDT_ENTRY(lpdt_token_logprobs_bwd), LPDT_ENTRY(lpdt_distill_topk)};
 constexpr int kNumEntries = (int)(sizeof(kEntries) / sizeof(kEntries[0]));
 
 }  // namespace lpdt

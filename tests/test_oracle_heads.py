@@ -77,3 +77,88 @@ def test_product_refusals():
                 dict(c_row=4), dict(c_node=14), dict(bias=P, bias_node=-1), dict(bias=P + 2)):
         assert call(**bad) == INVALID, bad
     assert call(K=(1 << 30) + 1) == UNSUPPORTED and call(M=1 << 31, c_node=1 << 40) == UNSUPPORTED
+
+
+# ------------------------------------------------------------------ reports and losses
+def test_logprobs_by_hand():
+    x = np.array([[0.0, np.log(3.0), -np.inf], [2.0, 2.0, 2.0], [-np.inf] * 3])
+    o = heads.token_logprobs(x, np.array([1, -1, 0]), 1.0, 2)
+    assert np.allclose(o["lse"][:2], [np.log(4), 2 + np.log(3)]) and o["lse"][2] == -np.inf
+    assert np.allclose(o["logprob"], [np.log(0.75), 0, -np.inf]) and np.allclose(o["entropy"], [np.log(4) - 0.75 * np.log(3), np.log(3), 0])
+    assert o["top_index"].tolist() == [[1, 0], [0, 1], [0, 1]] and np.allclose(o["top_logprob"][0], np.log([0.75, 0.25]))
+
+
+def difference(f, x, step=1e-5):
+    g = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        up, down = x.copy(), x.copy()
+        up[i] += step
+        down[i] -= step
+        g[i] = (f(up) - f(down)) / (2 * step)
+    return g
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.6])
+def test_logprobs_gradient_by_differences(temperature):
+    rng = np.random.default_rng(0)
+    x, tokens = rng.standard_normal((3, 7)) * 2, np.array([2, -1, 6])
+    g, h, l = rng.standard_normal((3, 3))
+    f = lambda x: sum((w * heads.token_logprobs(x, tokens, temperature)[n]).sum() for w, n in ((g, "logprob"), (h, "entropy"), (l, "lse")))
+    assert np.allclose(heads.token_logprobs_bwd(x, tokens, g, h, l, temperature), difference(f, x), atol=1e-8)
+
+
+@pytest.mark.parametrize("tail", [True, False])
+def test_distillation_by_hand_and_by_differences(tail):
+    """Two listed of three tokens; a token listed twice, a short list, no list, a row of weight 0."""
+    x = np.log(np.array([[[0.5, 0.3, 0.2]]]))
+    value, index = np.log(np.array([[[0.6, 0.1]]])), np.array([[[0, 2]]])
+    t = np.array([0.6, 0.1, 0.3]) if tail else np.array([6 / 7, 1 / 7, 0])
+    p = np.array([0.5, 0.2, 0.3])
+    want = sum(a * np.log(a / b) for a, b in zip(t, p) if a)
+    loss, row, grad = heads.distill_topk(x, value, index, tail)
+    assert np.allclose([loss[0], row[0, 0]], want)
+    assert np.allclose(grad[0, 0], np.array([0.5 - t[0], 0.3 - t[2], 0.2 - t[1]]))
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((2, 3, 6))
+    index = rng.integers(0, 6, (2, 3, 4))
+    index[0, 1, 2:], index[0, 2], index[1, 0, 1] = -1, -1, index[1, 0, 0]
+    value = np.log(rng.dirichlet(np.ones(4), (2, 3)) * 0.8)
+    weight = np.array([[1.0, 2.0, 1.0], [0.5, 0.0, 3.0]])
+    f = lambda x: heads.distill_topk(x, value, index, tail, 0.7, weight)[0].sum()
+    assert np.allclose(heads.distill_topk(x, value, index, tail, 0.7, weight)[2], difference(f, x), atol=1e-8)
+
+
+def test_report_refusals():
+    names = "rows V x dtype stride temperature tokens logprob entropy lse k top index status stream".split()
+    base = dict(rows=3, V=9, x=P, dtype=0, stride=9, temperature=1.0, tokens=P, logprob=P, entropy=P, lse=P, k=2, top=P, index=P, status=0, stream=0)
+    call = lambda **kw: _lib.lib().lpdt_token_logprobs(*[{**base, **kw}[n] for n in names])
+    assert call(rows=0) == OK and call(rows=0, x=0) == OK
+    for bad in (dict(rows=-1), dict(V=0), dict(V=-3), dict(x=0), dict(dtype=9), dict(stride=8), dict(temperature=0.0), dict(temperature=-1.0),
+                dict(temperature=float("nan")), dict(temperature=float("inf")), dict(tokens=0), dict(k=10), dict(k=-1), dict(top=0),
+                dict(index=0), dict(logprob=0, entropy=0, lse=0, k=0), dict(x=P + 2), dict(x=P + 1, dtype=2)):
+        assert call(**bad) == INVALID, bad
+    assert call(k=129, V=200, stride=200) == UNSUPPORTED and call(V=(1 << 30) + 1, stride=1 << 31) == UNSUPPORTED and call(rows=1 << 28) == UNSUPPORTED
+
+
+def test_report_gradient_refusals():
+    names = "rows V x dtype stride temperature tokens lse entropy g h l dx dstride stream".split()
+    base = dict(rows=3, V=9, x=P, dtype=0, stride=9, temperature=1.0, tokens=P, lse=P, entropy=P, g=P, h=P, l=P, dx=P * 2, dstride=9, stream=0)
+    call = lambda **kw: _lib.lib().lpdt_token_logprobs_bwd(*[{**base, **kw}[n] for n in names])
+    assert call(rows=0) == OK
+    for bad in (dict(rows=-1), dict(V=0), dict(x=0), dict(dx=0), dict(lse=0), dict(tokens=0), dict(entropy=0), dict(g=0, h=0, l=0), dict(dstride=8),
+                dict(stride=1), dict(dx=P, dstride=10), dict(dx=P + 1), dict(temperature=0.0), dict(dtype=3)):
+        assert call(**bad) == INVALID, bad
+    assert call(rows=1 << 28) == UNSUPPORTED
+
+
+def test_distillation_refusals():
+    names = "nodes B V x dtype stride temperature k value index tail weight loss row_loss dx dstride status stream".split()
+    base = dict(nodes=2, B=3, V=9, x=P, dtype=0, stride=9, temperature=1.0, k=2, value=P, index=P, tail=1, weight=0, loss=P, row_loss=P, dx=2 * P,
+                dstride=9, status=0, stream=0)
+    call = lambda **kw: _lib.lib().lpdt_distill_topk(*[{**base, **kw}[n] for n in names])
+    assert call(nodes=0) == OK
+    for bad in (dict(nodes=-1), dict(B=0), dict(V=0), dict(x=0), dict(value=0), dict(index=0), dict(loss=0), dict(row_loss=0), dict(k=0), dict(k=-2),
+                dict(tail=2), dict(stride=8), dict(dstride=3), dict(dx=P, dstride=12), dict(temperature=0.0), dict(temperature=float("nan")),
+                dict(dtype=-1), dict(x=P + 1), dict(dx=2 * P + 2)):
+        assert call(**bad) == INVALID, bad
+    assert call(k=129) == UNSUPPORTED and call(V=(1 << 20) + 1, stride=1 << 21, dstride=1 << 21) == UNSUPPORTED
