@@ -28,149 +28,194 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     return r;
 }
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) { return e4m3x2(a, b) | (e4m3x2(c, d) << 16); }
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// NV consecutive elements at p, of which the first `have` exist (the others read 0); VEC: p is aligned to all of them.
-template <typename T, int NV, bool VEC>
-__device__ __forceinline__ void load_some(const T *__restrict__ p, int have, float *f) {
-    constexpr int WORDS = NV * (int)sizeof(T) / 4, PER = 4 / (int)sizeof(T);
-    if (VEC && have >= NV) {
-        uint32_t w[WORDS];
-        if constexpr (WORDS == 4) {
+// NW words of consecutive elements at p, as they lie in memory; the first `have` elements exist, the others read 0.  VEC: p is aligned to
+// all of them.
+template <typename T, bool VEC, int NW>
+__device__ __forceinline__ void load_raw(const T *__restrict__ p, int have, uint32_t (&w)[NW]) {
+    constexpr int PER = 4 / (int)sizeof(T);
+    if (VEC && have >= NW * PER) {
+        if constexpr (NW == 4) {
             const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
         } else {
-            static_assert(WORDS == 2, "8 or 16 bytes");
+            static_assert(NW == 2, "8 or 16 bytes");
             const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
             w[0] = v.x; w[1] = v.y;
         }
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) unpack_word(w[i], f + i * PER, T());
     } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) f[i] = i < have ? to_f32(p[i]) : 0.f;
+        for (int i = 0; i < NW; ++i) {
+            float f[2];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) f[j] = i * PER + j < have ? to_f32(p[i * PER + j]) : 0.f;
+            w[i] = pack_word(f, T());
+        }
     }
+}
+// Maxima of |x| as bits: one value a word (fp32), or two side by side; then of the two, and as the bits of the same value in fp32.
+__device__ __forceinline__ uint32_t amax_word(uint32_t m, uint32_t w, float) { return max(m, w & 0x7fffffffu); }
+template <typename H> __device__ __forceinline__ uint32_t amax_word(uint32_t m, uint32_t w, H) { return __vmaxu2(m, w & 0x7fff7fffu); }
+__device__ __forceinline__ uint32_t amax_one(uint32_t m, float) { return m; }
+template <typename H> __device__ __forceinline__ uint32_t amax_one(uint32_t m, H) { return max(m >> 16, m & 0xffffu); }
+__device__ __forceinline__ uint32_t bits_f32(uint32_t b, float) { return b; }
+__device__ __forceinline__ uint32_t bits_f32(uint32_t b, __nv_bfloat16) { return b << 16; }
+__device__ __forceinline__ uint32_t bits_f32(uint32_t b, __half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)b))); }
+// The elements of a word times a power of two each (exact; what falls below the smallest normal number is below any code's half).
+__device__ __forceinline__ void scaled(uint32_t w, float s0, float, float *f, float) { f[0] = __uint_as_float(w) * s0; }
+__device__ __forceinline__ void scaled(uint32_t w, float s0, float s1, float *f, __half) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    f[0] = v.x * s0;
+    f[1] = v.y * s1;
+}
+__device__ __forceinline__ void scaled(uint32_t w, float s0, float s1, float *f, __nv_bfloat16) {
+    f[0] = __uint_as_float(w << 16) * s0;
+    f[1] = __uint_as_float(w & 0xffff0000u) * s1;
 }
 
 struct E4m3Args {
     const void *x;
     long long x_node, x_row;                      // strides in elements
     int rows, cols, nb, nbt;                      // blocks of a row, of a column
+    int chunks;                                   // of a row, for the warps of the rows' kernel
     uint8_t *q, *s, *qt, *st;
     int qp, sp, qtp, stp;                         // pitches in bytes
 };
 
-// Rows only.  128 / NV lanes hold a block, 16 bytes of the row each; U blocks in flight per lane.
+// Rows only.  128 / NV lanes hold a block, 16 bytes of the row each; a warp takes U times as many neighbouring blocks of one row.
 template <typename T, bool VEC, int U>
-__global__ void __launch_bounds__(256) quantize_e4m3_rows_kernel(const E4m3Args a, unsigned total) {
-    constexpr int NV = 16 / (int)sizeof(T), L = kBlk / NV, PER_CTA = 256 / L;
+__global__ void __launch_bounds__(256) quantize_e4m3_rows_kernel(const E4m3Args a, unsigned items) {
+    constexpr int NV = 16 / (int)sizeof(T), L = kBlk / NV, PER_WARP = 32 / L;
     pdl_enter();
-    const int k = threadIdx.x % L;
-    unsigned blk = blockIdx.x * (PER_CTA * U) + threadIdx.x / L;
-    float f[U][NV];
-    unsigned row[U], b[U];
+    const unsigned item = blockIdx.x * 8u + (threadIdx.x >> 5);
+    if (item >= items) return;
+    const unsigned row = item / (unsigned)a.chunks, n = row / (unsigned)a.rows, r = row - n * (unsigned)a.rows;      // row: over all nodes
+    const int lane = threadIdx.x & 31, k = lane % L;
+    const int b0 = (int)(item - row * (unsigned)a.chunks) * (PER_WARP * U) + lane / L;
+    const T *x = (const T *)a.x + n * a.x_node + r * a.x_row + k * NV;
+    uint8_t *q = a.q + (size_t)row * a.qp + k * NV, *s = a.s + (size_t)row * a.sp;
+    uint32_t w[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const unsigned at = blk + u * PER_CTA;
-        row[u] = at / (unsigned)a.nb;             // over all nodes
-        b[u] = at - row[u] * (unsigned)a.nb;
-        const unsigned n = row[u] / (unsigned)a.rows, r = row[u] - n * (unsigned)a.rows;
-        const int c = (int)b[u] * kBlk + k * NV;
-        const T *p = (const T *)a.x + n * a.x_node + r * a.x_row + c;
-        load_some<T, NV, VEC>(p, at < total ? a.cols - c : 0, f[u]);
+        const int c = (b0 + u * PER_WARP) * kBlk;
+        load_raw<T, VEC>(x + c, a.cols - c - k * NV, w[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const unsigned at = blk + u * PER_CTA;
         uint32_t amax = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) amax = max(amax, abs_bits(f[u][i]));
+        for (int i = 0; i < 4; ++i) amax = amax_word(amax, w[u][i], T());
+        amax = amax_one(amax, T());
 #pragma unroll
         for (int o = L / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        float inv;
-        const uint32_t s = block_scale(amax, inv);
-        if (at >= total) continue;
-        if (k == 0) a.s[(size_t)row[u] * a.sp + b[u]] = (uint8_t)s;
-        const int c = (int)b[u] * kBlk + k * NV;
-        if (c >= a.qp) continue;
-        uint8_t *q = a.q + (size_t)row[u] * a.qp + c;
-        uint32_t w[NV / 4];
+        float inv, f[NV];
+        const uint32_t scale = block_scale(bits_f32(amax, T()), inv);
+        const int b = b0 + u * PER_WARP;
+        if (k == 0 && b < a.nb) s[b] = (uint8_t)scale;
+        if (b * kBlk + k * NV >= a.qp) continue;
+        uint32_t c[NV / 4];
 #pragma unroll
-        for (int i = 0; i < NV / 4; ++i)
-            w[i] = e4m3x4(f[u][4 * i] * inv, f[u][4 * i + 1] * inv, f[u][4 * i + 2] * inv, f[u][4 * i + 3] * inv);
-        if constexpr (NV == 4) *reinterpret_cast<uint32_t *>(q) = w[0];
-        else *reinterpret_cast<uint2 *>(q) = make_uint2(w[0], w[1]);
+        for (int i = 0; i < 4; ++i) scaled(w[u][i], inv, inv, f + i * (NV / 4), T());
+#pragma unroll
+        for (int i = 0; i < NV / 4; ++i) c[i] = e4m3x4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+        if constexpr (NV == 4) *reinterpret_cast<uint32_t *>(q + b * kBlk) = c[0];
+        else *reinterpret_cast<uint2 *>(q + b * kBlk) = make_uint2(c[0], c[1]);
     }
 }
 
-// A tile of 128 x 128 values, both forms (or the transposed one alone).  A warp holds 16 rows, a lane four columns of them: the
-// 16 codes that a lane has of a column are 16 neighbouring bytes of the transposed form, turned through shared memory so that they leave
-// in rows of 128 bytes.
+// A tile of 128 x 128 values, both forms (or the transposed one alone).  A warp holds R rows, a lane four columns of them as they
+// came: the R codes that a lane has of a column are R neighbouring bytes of the transposed form, turned through shared memory so that
+// they leave in rows of 128 bytes.  R = 16 rows of 16-bit elements or 8 of fp32 are 32 registers, which leaves room for as many CTAs as
+// keep memory busy while others compute.
+template <typename T> struct TileShape {
+    static constexpr int R = 32 / (int)sizeof(T), THREADS = kBlk / R * 32, MIN_CTAS = 1024 / THREADS;
+};
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) quantize_e4m3_tile_kernel(const E4m3Args a) {
-    __shared__ uint32_t s_col[8][kBlk];
-    __shared__ uint4 s_t[kBlk][8];
+__global__ void __launch_bounds__(TileShape<T>::THREADS, TileShape<T>::MIN_CTAS) quantize_e4m3_tile_kernel(const E4m3Args a) {
+    constexpr int W = (int)sizeof(T), PER = 4 / W;             // words of four elements, elements of a word
+    constexpr int R = TileShape<T>::R, GROUPS = kBlk / R;
+    __shared__ uint32_t s_col[4][32];                          // [column % 4][column / 4]
+    __shared__ __align__(16) uint8_t s_t[kBlk][kBlk];          // [column][row], groups of R rows exchanged by column
     pdl_enter();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int r0 = blockIdx.y * kBlk + warp * 16, c0 = blockIdx.x * kBlk + lane * 4;
+    const int r0 = blockIdx.y * kBlk + warp * R, c0 = blockIdx.x * kBlk + lane * 4;
     const size_t node = blockIdx.z;
-    const T *x = (const T *)a.x + node * a.x_node + c0;
-    float f[16][4];
+    const T *x = (const T *)a.x + node * a.x_node + (long long)r0 * a.x_row + c0;
+    uint32_t w[R][W];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        load_some<T, 4, VEC>(x + (long long)(r0 + i) * a.x_row, r0 + i < a.rows ? a.cols - c0 : 0, f[i]);
-    uint32_t cm[4] = {0u, 0u, 0u, 0u};
+    for (int i = 0; i < R; ++i)
+        load_raw<T, VEC>(x + i * a.x_row, r0 + i < a.rows ? a.cols - c0 : 0, w[i]);
+    if (threadIdx.x < kBlk) (&s_col[0][0])[threadIdx.x] = 0u;
+    __syncthreads();
+    uint32_t cm[W];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int k = 0; k < W; ++k) cm[k] = 0u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) cm[j] = max(cm[j], abs_bits(f[i][j]));
-    *reinterpret_cast<uint4 *>(&s_col[warp][lane * 4]) = make_uint4(cm[0], cm[1], cm[2], cm[3]);
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int k = 0; k < W; ++k) cm[k] = amax_word(cm[k], w[i][k], T());
+#pragma unroll
+    for (int j = 0; j < 4; ++j) atomicMax(&s_col[j][lane], PER == 1 ? cm[j % W] : (j & 1) ? cm[j >> 1] >> 16 : cm[j >> 1] & 0xffffu);
     if (a.q) {
+        // lane i keeps row i's maximum, so the scales of all rows are one computation
+        uint32_t mine = 0u;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            uint32_t amax = max(max(abs_bits(f[i][0]), abs_bits(f[i][1])), max(abs_bits(f[i][2]), abs_bits(f[i][3])));
-            amax = __reduce_max_sync(0xffffffffu, amax);
-            float inv;
-            const uint32_t s = block_scale(amax, inv);
-            if (r0 + i >= a.rows) continue;
-            const size_t row = node * a.rows + r0 + i;
-            if (lane == 0) a.s[row * a.sp + blockIdx.x] = (uint8_t)s;
-            if (c0 < a.qp)
-                *reinterpret_cast<uint32_t *>(a.q + row * a.qp + c0) = e4m3x4(f[i][0] * inv, f[i][1] * inv, f[i][2] * inv, f[i][3] * inv);
+        for (int i = 0; i < R; ++i) {
+            uint32_t amax = 0u;
+#pragma unroll
+            for (int k = 0; k < W; ++k) amax = amax_word(amax, w[i][k], T());
+            amax = __reduce_max_sync(0xffffffffu, amax_one(amax, T()));
+            if (lane == i) mine = amax;
+        }
+        float inv;
+        const uint32_t scale = block_scale(bits_f32(mine, T()), inv);
+        const size_t row = node * a.rows + r0;
+        if (lane < R && r0 + lane < a.rows) a.s[(row + lane) * a.sp + blockIdx.x] = (uint8_t)scale;
+        uint8_t *q = a.q + row * a.qp + c0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float s = __shfl_sync(0xffffffffu, inv, i);
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < W; ++k) scaled(w[i][k], s, s, f + k * PER, T());
+            if (r0 + i < a.rows && c0 < a.qp) *reinterpret_cast<uint32_t *>(q) = e4m3x4(f[0], f[1], f[2], f[3]);
+            q += a.qp;
         }
     }
     __syncthreads();
     float inv[4];
-    uint32_t sc[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) cm[j] = 0u;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(&s_col[w][lane * 4]);
-        cm[0] = max(cm[0], v.x); cm[1] = max(cm[1], v.y); cm[2] = max(cm[2], v.z); cm[3] = max(cm[3], v.w);
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t s = block_scale(bits_f32(s_col[j][lane], T()), inv[j]);
+        if (warp == j && c0 + j < a.cols) a.st[(node * a.cols + c0 + j) * a.stp + blockIdx.y] = (uint8_t)s;
     }
+    uint32_t t[4][R / 4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sc[j] = block_scale(cm[j], inv[j]);
-    if (warp == 0) {
+    for (int h = 0; h < R / 4; ++h) {
+        float f[4][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c0 + j < a.cols) a.st[(node * a.cols + c0 + j) * a.stp + blockIdx.y] = (uint8_t)sc[j];
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < W; ++k) scaled(w[4 * h + i][k], inv[k * PER], inv[k * PER + PER - 1], f[i] + k * PER, T());
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j][h] = e4m3x4(f[0][j], f[1][j], f[2][j], f[3][j]);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = e4m3x4(f[4 * i][j] * inv[j], f[4 * i + 1][j] * inv[j], f[4 * i + 2][j] * inv[j], f[4 * i + 3][j] * inv[j]);
-        s_t[lane * 4 + j][warp ^ (lane & 7)] = make_uint4(w[0], w[1], w[2], w[3]);
+        uint8_t *to = &s_t[lane * 4 + j][(warp ^ (lane & (GROUPS - 1))) * R];
+        if constexpr (R == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(t[j][0], t[j][1]);
+        else *reinterpret_cast<uint4 *>(to) = make_uint4(t[j][0], t[j][1], t[j][2], t[j][3]);
     }
     __syncthreads();
-    const int tr = blockIdx.y * kBlk + (threadIdx.x & 7) * 16;
+    const int piece = threadIdx.x & 7, tr = blockIdx.y * kBlk + piece * 16;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = (threadIdx.x >> 3) + 32 * i, col = blockIdx.x * kBlk + c;
-        if (col < a.cols && tr < a.qtp)
-            *reinterpret_cast<uint4 *>(a.qt + (node * a.cols + col) * a.qtp + tr) = s_t[c][(threadIdx.x & 7) ^ ((c >> 2) & 7)];
+    for (int c = threadIdx.x >> 3; c < kBlk; c += TileShape<T>::THREADS / 8) {
+        const int col = blockIdx.x * kBlk + c, swz = (c >> 2) & (GROUPS - 1);
+        if (col < a.cols && tr < a.qtp) {
+            uint4 v = *reinterpret_cast<const uint4 *>(&s_t[c][R == 8 ? ((2 * piece) ^ (swz & 14)) * 8 : (piece ^ swz) * 16]);
+            if (R == 8 && (swz & 1)) v = make_uint4(v.z, v.w, v.x, v.y);
+            *reinterpret_cast<uint4 *>(a.qt + (node * a.cols + col) * a.qtp + tr) = v;
+        }
     }
 }
 
@@ -204,23 +249,23 @@ extern "C" lpdt_status lpdt_quantize_e4m3(const void *x, lpdt_dtype dtype, int32
     return with_dtype(dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
         if (!qt) {
-            constexpr int NV = 16 / (int)sizeof(T), PER_CTA = 256 / (kBlk / NV);
+            constexpr int NV = 16 / (int)sizeof(T), PER_WARP = 32 / (kBlk / NV);
             const bool vec = aligned(x, 16) && (a.x_row % NV == 0) && (a.x_node % NV == 0);
-            const int64_t total = (int64_t)nodes * rows * a.nb;
-            if (total > (int64_t)0x7fffffff) return LPDT_ERR_UNSUPPORTED;
-            if (total >= 4 * PER_CTA * kNumSMs)
-                launch_k(vec ? quantize_e4m3_rows_kernel<T, true, 4> : quantize_e4m3_rows_kernel<T, false, 4>,
-                                   (unsigned)ceil_div(total, PER_CTA * 4), 256, 0, st, a, (unsigned)total);
-            else
-                launch_k(vec ? quantize_e4m3_rows_kernel<T, true, 1> : quantize_e4m3_rows_kernel<T, false, 1>,
-                                   (unsigned)ceil_div(total, PER_CTA), 256, 0, st, a, (unsigned)total);
+            const int64_t all = (int64_t)nodes * rows;
+            if (all * a.nb > (int64_t)0x7fffffff) return LPDT_ERR_UNSUPPORTED;
+            // four groups of blocks a warp once that leaves every SM some 32 warps
+            const bool four = all * ceil_div(a.nb, 4 * PER_WARP) >= 32 * kNumSMs;
+            a.chunks = (int)ceil_div(a.nb, (four ? 4 : 1) * PER_WARP);
+            const unsigned items = (unsigned)(all * a.chunks), grid = (unsigned)ceil_div(items, 8);
+            if (four) launch_k(vec ? quantize_e4m3_rows_kernel<T, true, 4> : quantize_e4m3_rows_kernel<T, false, 4>, grid, 256, 0, st, a, items);
+            else launch_k(vec ? quantize_e4m3_rows_kernel<T, true, 1> : quantize_e4m3_rows_kernel<T, false, 1>, grid, 256, 0, st, a, items);
             LPDT_LAUNCH_CHECK();
             return LPDT_OK;
         }
         const bool vec = aligned(x, 4 * sizeof(T)) && a.x_row % 4 == 0 && a.x_node % 4 == 0;
         if (a.nbt > 65535 || nodes > 65535) return LPDT_ERR_UNSUPPORTED;
         launch_k(vec ? quantize_e4m3_tile_kernel<T, true> : quantize_e4m3_tile_kernel<T, false>,
-                           dim3((unsigned)a.nb, (unsigned)a.nbt, (unsigned)nodes), 256, 0, st, a);
+                           dim3((unsigned)a.nb, (unsigned)a.nbt, (unsigned)nodes), TileShape<T>::THREADS, 0, st, a);
         LPDT_LAUNCH_CHECK();
         return LPDT_OK;
     });

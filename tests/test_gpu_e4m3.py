@@ -68,8 +68,10 @@ def edge_values():
     return torch.from_numpy(x)[None]
 
 
-def test_quantize_at_its_edges():
-    x = edge_values().cuda()
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_quantize_at_its_edges(dtype):
+    x = edge_values()
+    x = (x if dtype != torch.float16 else x.clamp(-60000, 60000) * 2.0 ** -8).to(dtype).cuda()
     check_quantized(x, quantize(x))
     check_quantized(x, quantize(x, both=False))
     t = x.transpose(1, 2).contiguous()
