@@ -131,7 +131,7 @@ __device__ __forceinline__ float listed_grad(const DistillArgs &a, const List &l
 
 template <typename T>
 __global__ void __launch_bounds__(kDtThreads) distill_row_kernel(const DistillArgs a) {
-    constexpr int VE = Row<T>::VE, U = kDtUnroll, PER = 4 / (int)sizeof(T);
+    constexpr int VE = Row<T>::VE, U = kDtUnroll;
     extern __shared__ uint32_t s_bits[];              // a bit per position of this CTA's words: listed
     __shared__ List s_list;
     __shared__ Stats s_warp[kDtWarps];
@@ -142,52 +142,59 @@ __global__ void __launch_bounds__(kDtThreads) distill_row_kernel(const DistillAr
     const long long row = blockIdx.x / share;
     const Row<T> r((const T *)a.x + row * a.x_row, a.V);
     T *dx = a.dx ? (T *)a.dx + row * a.dx_row : nullptr;
-    const bool same = dx && ((uintptr_t)dx & 15) / sizeof(T) == (uintptr_t)r.head;
+    const bool same = ((uintptr_t)(dx + r.head) & 15) == 0;
     const int begin = (int)((long long)r.words * rank / share), end = (int)((long long)r.words * (rank + 1) / share);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float weight = a.weight ? a.weight[row] : 1.f;
     const double g = (double)weight * a.inv_t / (double)a.B;
     const bool skip = weight == 0.f;                  // the same for the whole cluster
+    const int edge = rank == 0 && threadIdx.x < Row<T>::EDGES ? r.edge(threadIdx.x) : -1;
+    float at_edge = -INFINITY;
 
     Stats st;
     st.reset();
     if (!skip) {
-        const int bit_words = (int)(((long long)(end - begin) * VE + 31) / 32);
+        const int bit_words = ((end - begin) * VE + 31) / 32;
         for (int i = threadIdx.x; i < bit_words; i += kDtThreads) s_bits[i] = 0;
         if (warp == 0) make_list<T>(a, row, s_list, lane, rank == 0);
         __syncthreads();
         if ((int)threadIdx.x < a.k && s_list.id[threadIdx.x] >= 0) {
-            const long long at = (long long)s_list.id[threadIdx.x] + r.head - (long long)begin * VE;
-            if (at >= 0 && at < (long long)(end - begin) * VE) atomicOr(&s_bits[at >> 5], 1u << (at & 31));
+            const int at = s_list.id[threadIdx.x] - r.index(begin);
+            if (at >= 0 && at < (end - begin) * VE) atomicOr(&s_bits[at >> 5], 1u << (at & 31));
+        }
+        if (edge >= 0) {
+            at_edge = to_f32(r.at(edge));
+            bool out = false;
+            for (int j = 0; j < a.k; ++j) out |= s_list.id[j] == edge;
+            const float x[2] = {out ? -INFINITY : at_edge, -INFINITY};
+            if (x[0] > st.m) st.raise(x[0], a.c);
+            accumulate<2, false>(st, x, a.c);
         }
         __syncthreads();
         const uint8_t *bytes = reinterpret_cast<const uint8_t *>(s_bits);
-        for (int w0 = begin; w0 < end; w0 += kDtThreads * U) {
+        auto word = [&](const uint4 &v, int i0) {
+            float f[VE];
+            unpack_vec<T>(v, f);
+            const uint32_t out = VE == 8 ? bytes[i0] : (bytes[i0 >> 1] >> (4 * (i0 & 1))) & 15u;
+            if (out) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) if ((out >> i) & 1u) f[i] = -INFINITY;
+            }
+            float m = f[0];
+#pragma unroll
+            for (int i = 1; i < VE; ++i) m = fmaxf(m, f[i]);
+            if (m > st.m) st.raise(m, a.c);
+            accumulate<VE, false>(st, f, a.c);
+        };
+        int w = begin + (int)threadIdx.x;
+        for (; w + (U - 1) * kDtThreads < end; w += kDtThreads * U) {
             uint4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = w0 + u * kDtThreads + (int)threadIdx.x;
-                if (at < end) v[u] = r.load(at, from_f32<T>(-INFINITY));
-            }
+            for (int u = 0; u < U; ++u) v[u] = r.load(w + u * kDtThreads);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = w0 + u * kDtThreads + (int)threadIdx.x;
-                if (at >= end) continue;
-                float f[VE];
-                unpack_vec<T>(v[u], f);
-                const int i0 = at - begin;
-                const uint32_t out = VE == 8 ? bytes[i0] : (bytes[i0 >> 1] >> (4 * (i0 & 1))) & 15u;
-                if (out) {
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) if ((out >> i) & 1u) f[i] = -INFINITY;
-                }
-                float m = f[0];
-#pragma unroll
-                for (int i = 1; i < VE; ++i) m = fmaxf(m, f[i]);
-                if (m > st.m) st.raise(m, a.c);
-                accumulate<VE, false>(st, f, a.c);
-            }
+            for (int u = 0; u < U; ++u) word(v[u], w + u * kDtThreads - begin);
         }
+        for (; w < end; w += kDtThreads) word(r.load(w), w - begin);
         warp_join(st, a.c);
         if (lane == 0) s_warp[warp] = st;
         __syncthreads();
@@ -236,43 +243,43 @@ __global__ void __launch_bounds__(kDtThreads) distill_row_kernel(const DistillAr
         __syncthreads();
     }
     const float rest = skip ? 0.f : s_terms.rest, m = skip ? 0.f : s_warp[0].m;
-    for (int w0 = begin; w0 < end; w0 += kDtThreads * U) {
-        uint4 v[U];
+    auto grad = [&](float x) { return rest * ex2(max_nan((x - m) * a.c, kFar)); };
+    auto put = [&](int w, const float *f) {
+        if (same) *reinterpret_cast<uint4 *>(dx + r.index(w)) = pack_vec<T>(f);
+        else {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = w0 + u * kDtThreads + (int)threadIdx.x;
-            if (at < end && !skip) v[u] = r.load(at, from_f32<T>(0.f));
+            for (int i = 0; i < VE; ++i) dx[r.index(w) + i] = from_f32<T>(f[i]);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = w0 + u * kDtThreads + (int)threadIdx.x;
-            if (at >= end) continue;
+    };
+    int w = begin + (int)threadIdx.x;
+    if (!skip) {
+        auto word = [&](const uint4 &v, int at) {
             float f[VE];
-            if (skip) {
+            unpack_vec<T>(v, f);
 #pragma unroll
-                for (int i = 0; i < VE; ++i) f[i] = 0.f;
-            } else {
-                unpack_vec<T>(v[u], f);
+            for (int i = 0; i < VE; ++i) f[i] = grad(f[i]);
+            put(at, f);
+        };
+        for (; w + (U - 1) * kDtThreads < end; w += kDtThreads * U) {
+            uint4 v[U];
 #pragma unroll
-                for (int i = 0; i < VE; ++i) f[i] = rest * ex2(max_nan((f[i] - m) * a.c, kFar));
-            }
-            const int first = at * VE - r.head;
-            if (same && r.whole(at)) {
-                *reinterpret_cast<uint4 *>(dx + first) =
-                    make_uint4(pack_word(f, T()), pack_word(f + PER, T()), pack_word(f + 2 * PER, T()), pack_word(f + 3 * PER, T()));
-            } else {
+            for (int u = 0; u < U; ++u) v[u] = r.load(w + u * kDtThreads);
 #pragma unroll
-                for (int i = 0; i < VE; ++i)
-                    if (r.holds((long long)at * VE + i)) dx[first + i] = from_f32<T>(f[i]);
-            }
+            for (int u = 0; u < U; ++u) word(v[u], w + u * kDtThreads);
         }
+        for (; w < end; w += kDtThreads) word(r.load(w), w);
+    } else {
+        const float zeros[VE] = {};
+        for (; w < end; w += kDtThreads) put(w, zeros);
     }
+    if (edge >= 0) dx[edge] = from_f32<T>(skip ? 0.f : grad(at_edge));
     if (skip) return;
     __syncthreads();
     if ((int)threadIdx.x < a.k && s_list.first[threadIdx.x]) {
-        const long long at = (long long)s_list.id[threadIdx.x] + r.head;
-        if (at >= (long long)begin * VE && at < (long long)end * VE)
-            dx[s_list.id[threadIdx.x]] = from_f32<T>(listed_grad(a, s_list, s_terms, g, threadIdx.x));
+        const int id = s_list.id[threadIdx.x], at = id - r.index(begin);
+        const bool here = (at >= 0 && at < (end - begin) * VE) || (rank == 0 && (id < r.head || id >= r.index(r.words)));
+        if (here)
+            dx[id] = from_f32<T>(listed_grad(a, s_list, s_terms, g, threadIdx.x));
     }
 }
 

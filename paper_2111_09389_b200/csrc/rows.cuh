@@ -1,9 +1,8 @@
 // Rows of logits, read once: 16-byte accesses at any alignment of the row, the running maximum and sums of a softmax, and their
 // joining across lanes, warps and the CTAs of a cluster.  Not part of the ABI.
 //
-// A row of V elements at p is seen as the 16-byte words of memory that it touches: position = index + head, head = elements of the
-// first word before the row.  A first or last word that holds others' elements is read element by element, so nothing outside the
-// row is touched and a row stride of any parity costs two short accesses per row.
+// A row of V elements is seen as the 16-byte words of memory that lie wholly inside it, and fewer than 16 bytes before and behind them (the
+// edges), which are read element by element: nothing outside the row is touched, and a row may start anywhere.
 #pragma once
 #include <math.h>
 #include "dtypes.cuh"
@@ -20,7 +19,14 @@ __device__ __forceinline__ uint32_t rows_cluster_size() { uint32_t r; asm volati
 __device__ __forceinline__ void rows_cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// The value at the same place of shared memory in the CTA of that rank.
+__device__ __forceinline__ void rows_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void rows_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// To and from the same place of shared memory in the CTA of that rank.
+__device__ __forceinline__ void st_peer_u64(void *local, uint32_t rank, unsigned long long v) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+}
 __device__ __forceinline__ unsigned long long ld_peer_u64(const void *local, uint32_t rank) {
     uint32_t a;
     unsigned long long v;
@@ -31,24 +37,24 @@ __device__ __forceinline__ unsigned long long ld_peer_u64(const void *local, uin
 
 template <typename T>
 struct Row {
-    static constexpr int VE = 16 / (int)sizeof(T);
-    const T *base;           // 16-byte aligned; position 0
-    int head, V, words;      // words of 16 bytes that the row touches
+    static constexpr int VE = 16 / (int)sizeof(T), EDGES = 2 * (VE - 1);
+    const T *base;           // of word 0, 16-byte aligned
+    int head, V, words;      // elements before word 0; words
     __device__ __forceinline__ Row(const T *p, int V_) : V(V_) {
-        head = (int)(((uintptr_t)p & 15) / sizeof(T));
-        base = p - head;
-        words = (int)(((long long)head + V + VE - 1) / VE);
+        head = (int)((16 - ((uintptr_t)p & 15)) % 16 / sizeof(T));
+        if (head > V) head = V;
+        base = p + head;
+        words = (V - head) / VE;
     }
-    __device__ __forceinline__ bool whole(int w) const { return (w > 0 || head == 0) && (long long)(w + 1) * VE <= (long long)head + V; }
-    __device__ __forceinline__ bool holds(long long pos) const { return pos >= head && pos < (long long)head + V; }
-    // Elements of word w as bits; those outside the row are `fill`.
-    __device__ __forceinline__ uint4 load(int w, T fill) const {
-        if (whole(w)) return reinterpret_cast<const uint4 *>(base)[w];
-        union { uint4 v; T e[VE]; } u;
-#pragma unroll
-        for (int i = 0; i < VE; ++i) u.e[i] = holds((long long)w * VE + i) ? base[(long long)w * VE + i] : fill;
-        return u.v;
+    __device__ __forceinline__ uint4 load(int w) const { return reinterpret_cast<const uint4 *>(base)[w]; }
+    __device__ __forceinline__ int index(int w) const { return w * VE + head; }          // of the word's first element
+    // Index of the i-th element of the edges (i < EDGES), -1 where there is none.
+    __device__ __forceinline__ int edge(int i) const {
+        if (i < VE - 1) return i < head ? i : -1;
+        const int v = head + words * VE + i - (VE - 1);
+        return v < V ? v : -1;
     }
+    __device__ __forceinline__ T at(int i) const { return (base - head)[i]; }
 };
 template <typename T> __device__ __forceinline__ void unpack_vec(const uint4 &v, float *f) {
     constexpr int PER = 4 / (int)sizeof(T);
@@ -56,6 +62,33 @@ template <typename T> __device__ __forceinline__ void unpack_vec(const uint4 &v,
     unpack_word(v.y, f + PER, T());
     unpack_word(v.z, f + 2 * PER, T());
     unpack_word(v.w, f + 3 * PER, T());
+}
+
+template <typename T> __device__ __forceinline__ uint4 pack_vec(const float *f) {
+    constexpr int PER = 4 / (int)sizeof(T);
+    return make_uint4(pack_word(f, T()), pack_word(f + PER, T()), pack_word(f + 2 * PER, T()), pack_word(f + 3 * PER, T()));
+}
+
+// The largest of a word's elements, NaN passed over; a word of nothing but NaN may answer NaN.
+__device__ __forceinline__ float vec_max_of(const uint4 &v, float) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+}
+__device__ __forceinline__ float vec_max_of(const uint4 &v, __nv_bfloat16) {
+    const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&v);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float vec_max_of(const uint4 &v, __half) {
+    const __half2 *h = reinterpret_cast<const __half2 *>(&v);
+    const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+template <typename T> __device__ __forceinline__ float vec_max(const uint4 &v) { return vec_max_of(v, T()); }
+// A word of one value throughout.
+__device__ __forceinline__ uint4 same_word(float f) { const uint32_t b = __float_as_uint(f); return make_uint4(b, b, b, b); }
+template <typename H> __device__ __forceinline__ uint4 same_word(H h) {
+    const uint32_t s = *reinterpret_cast<const unsigned short *>(&h), b = s | (s << 16);
+    return make_uint4(b, b, b, b);
 }
 
 // Running sums relative to the maximum so far: s = sum 2^t, w = sum 2^t * t with t = (x - m) * c, c = log2(e) / temperature.
@@ -80,24 +113,40 @@ struct Stats {
         w += b.w;
     }
 };
-__device__ __forceinline__ Stats shfl_xor(const Stats &a, int o) {
-    Stats b;
-    b.m = __shfl_xor_sync(0xffffffffu, a.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, a.s, o);
-    b.w = __shfl_xor_sync(0xffffffffu, a.w, o);
-    return b;
+// The largest of the lanes' numbers.
+__device__ __forceinline__ float warp_max_f(float v) {
+    const uint32_t b = __float_as_uint(v), o = __reduce_max_sync(0xffffffffu, b ^ ((uint32_t)((int)b >> 31) | 0x80000000u));
+    return __uint_as_float(o ^ ((uint32_t)(~(int)o >> 31) | 0x80000000u));
 }
+// Joins the lanes' sums: to their maximum first, then they add.
 __device__ __forceinline__ void warp_join(Stats &a, float c) {
+    a.raise(warp_max_f(a.m), c);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) a.join(shfl_xor(a, o), c);
+    for (int o = 16; o > 0; o >>= 1) {
+        a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+        a.w += __shfl_xor_sync(0xffffffffu, a.w, o);
+    }
 }
-// Adds a word's elements; the maximum has been raised to cover them.
+// Adds a word's elements, two at a time; the maximum has been raised to cover them.
 template <int N, bool W> __device__ __forceinline__ void accumulate(Stats &a, const float *f, float c) {
+    const F2 minus_m = pack2(-a.m, -a.m), c2 = pack2(c, c);
+    F2 s = pack2(a.s, 0.f), w = pack2(a.w, 0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float t = max_nan((f[i] - a.m) * c, kFar), e = ex2(t);
-        a.s += e;
-        if (W) a.w = fmaf(e, t, a.w);
+    for (int i = 0; i < N; i += 2) {
+        float t0, t1;
+        unpack2(mul2(add2(pack2(f[i], f[i + 1]), minus_m), c2), t0, t1);
+        t0 = max_nan(t0, kFar);
+        t1 = max_nan(t1, kFar);
+        const F2 e = pack2(ex2(t0), ex2(t1));
+        s = add2(s, e);
+        if (W) w = fma2(e, pack2(t0, t1), w);
+    }
+    float s0, s1;
+    unpack2(s, s0, s1);
+    a.s = s0 + s1;
+    if (W) {
+        unpack2(w, s0, s1);
+        a.w = s0 + s1;
     }
 }
 

@@ -3,10 +3,10 @@
 //
 // Memory is the bound: a row is read once.  Each thread keeps the running maximum m and, relative to it, s = sum 2^t and
 // w = sum 2^t * t; then lse = m/T + ln s and H = ln s - ln2 * w / s, without a second pass for the maximum or the entropy.
-// The top k come out of the same pass: the k-th largest of the threads' maxima over the first tile is a floor that the final k-th value
-// cannot lie under, so of the rest of the row only what reaches the floor is written to a list in shared memory; when the list has
-// grown, it is cut to its k best, which raises the floor.  Keys hold value and position, so equal values go to the lower position and
-// a row of nothing but equal values needs no more than its first k.
+// The top k come out of the same pass: a thread remembers the two of its turns (of four words of 16 bytes) with the largest maxima, which
+// costs a comparison a turn and no barrier.  At the end the threads' best elements give a floor that the k-th value cannot lie under, and what reaches it, a few
+// more than k, is written to a list in shared memory and ranked.  Keys hold value and position, so equal values go to the lower position
+// and a row of nothing but equal values needs no more than its first k.
 //
 // Few rows: the CTAs of a cluster share a row and join through distributed shared memory.  Rows of up to 1024 values: a warp each.
 #include "rows.cuh"
@@ -30,12 +30,12 @@ struct RowAnswer {
     __device__ __forceinline__ float of(float x) const {
         return none || x == -INFINITY ? (log_s != log_s ? NAN : -INFINITY) : (float)(((double)x - (double)m) * inv_t - log_s);
     }
+    RowAnswer() = default;
     __device__ __forceinline__ float lse() const { return none ? -INFINITY : (float)((double)m * inv_t + log_s); }
     __device__ __forceinline__ float entropy(const Stats &a) const { return none ? 0.f : (float)(log_s - kLn2 * (double)a.w / (double)a.s); }
 };
 template <typename T>
-__device__ __forceinline__ void answer_row(const LogprobArgs &a, long long row, const Stats &st) {
-    const RowAnswer r(st, a.inv_t);
+__device__ __forceinline__ void answer_row(const LogprobArgs &a, long long row, const Stats &st, const RowAnswer &r) {
     if (a.lse) a.lse[row] = r.lse();
     if (a.entropy) a.entropy[row] = r.entropy(st);
     if (a.logprob) {
@@ -47,212 +47,331 @@ __device__ __forceinline__ void answer_row(const LogprobArgs &a, long long row, 
     }
 }
 
-constexpr int kLpThreads = 256, kLpWarps = kLpThreads / 32, kLpUnroll = 4, kTopMax = 128, kTopCap = 2048;
+constexpr int kLpUnroll = 4, kTopMax = 128;
 
-struct TopList {
-    unsigned long long key[kTopCap];
+// What could be among the k best of a row, and then the k best in order.
+template <int TH> struct TopList {
+    static constexpr int CAP = TH < 256 ? 8 * TH : 2048;
+    __align__(16) unsigned long long key[CAP];
     int count;
 };
-// Cuts the list to its k best, in order.  Each thread ranks its share of the n keys by counting the larger ones.
-__device__ __forceinline__ void top_cut(TopList &l, int n, int k) {
-    constexpr int PER = kTopCap / kLpThreads;
-    unsigned long long mine[PER];
-    int rank[PER];
-    const int turns = (n + kLpThreads - 1) / kLpThreads;
+// Cuts the list of n keys to its k best, in order.  Each thread ranks its share by counting the larger ones: n is near k.
+template <int TH>
+__device__ __noinline__ void top_cut(TopList<TH> &l, int n, int k) {
+    constexpr int PER = TopList<TH>::CAP / TH;
+    if (n <= TH) {
+        const unsigned long long mine = (int)threadIdx.x < n ? l.key[threadIdx.x] : 0;
+        int r = TH;
+        if ((int)threadIdx.x < n) {
+            r = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) r += l.key[j] > mine;
+        }
+        __syncthreads();
+        if (r < k) l.key[r] = mine;
+    } else {
+        unsigned long long mine[PER];
+        int rank[PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int at = threadIdx.x + i * kLpThreads;
-        rank[i] = kTopCap;
-        if (i >= turns || at >= n) continue;
-        mine[i] = l.key[at];
-        int r = 0;
-        for (int j = 0; j < n; ++j) r += l.key[j] > mine[i];
-        rank[i] = r;
+        for (int i = 0; i < PER; ++i) {
+            const int at = threadIdx.x + i * TH;
+            rank[i] = TopList<TH>::CAP;
+            if (at >= n) continue;
+            mine[i] = l.key[at];
+            int r = 0;
+            for (int j = 0; j < n; ++j) r += l.key[j] > mine[i];
+            rank[i] = r;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (rank[i] < k) l.key[rank[i]] = mine[i];
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (rank[i] < k) l.key[rank[i]] = mine[i];
     if (threadIdx.x == 0) l.count = n < k ? n : k;
     __syncthreads();
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads) logprobs_row_kernel(const LogprobArgs a) {
-    constexpr int VE = Row<T>::VE, U = kLpUnroll;
-    __shared__ TopList s_top;
-    __shared__ Stats s_warp[kLpWarps];
+// The two turns of a thread (kLpUnroll words each, named by the first) with the largest maxima, of equal ones the earlier; NaN: none yet.
+struct Best {
+    float v1, v2;
+    int w1, w2;
+    __device__ __forceinline__ void reset() { v1 = v2 = NAN; w1 = w2 = -1; }
+    __device__ __forceinline__ void see(float x, int at) {
+        if (x != x) return;
+        const bool first = !(x <= v1);
+        v2 = first ? v1 : x;
+        w2 = first ? w1 : at;
+        v1 = first ? x : v1;
+        w1 = first ? at : w1;
+    }
+};
+// The best key of a word whose first element has this index (0: nothing but NaN); calls, so that the kernel around them keeps its registers.
+template <typename T>
+__device__ __noinline__ unsigned long long word_best(uint4 v, int index) {
+    constexpr int VE = Row<T>::VE;
+    float x[VE];
+    unpack_vec<T>(v, x);
+    unsigned long long best = 0;
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+        if (x[i] == x[i]) {
+            const unsigned long long key = top_key(x[i], index + i);
+            if (key > best) best = key;
+        }
+    return best;
+}
+template <typename T, int TH>
+__device__ __noinline__ void word_offer(uint4 v, int index, unsigned long long floor_key, float floor_v, TopList<TH> &l) {
+    constexpr int VE = Row<T>::VE;
+    float x[VE];
+    unpack_vec<T>(v, x);
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        if (!(x[i] >= floor_v)) continue;
+        const unsigned long long key = top_key(x[i], index + i);
+        if (key < floor_key) continue;
+        const int to = atomicAdd(&l.count, 1);
+        if (to < TopList<TH>::CAP) l.key[to] = key;
+    }
+}
+// A thread's turn from word w on; what is not there is `fill`.
+template <typename T, int TH>
+__device__ __forceinline__ void load_turn(const Row<T> &r, int w, int end, uint4 (&v)[kLpUnroll], float fill) {
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u) v[u] = w + u * TH < end ? r.load(w + u * TH) : same_word(from_f32<T>(fill));
+}
+template <typename T, int TH>
+__device__ __forceinline__ void offer(const Row<T> &r, int w, int end, unsigned long long floor_key, float floor_v, TopList<TH> &l) {
+    uint4 v[kLpUnroll];
+    load_turn<T, TH>(r, w, end, v, NAN);
+#pragma unroll
+    for (int u = 0; u < kLpUnroll; ++u)
+        if (vec_max<T>(v[u]) >= floor_v) word_offer<T, TH>(v[u], r.index(w + u * TH), floor_key, floor_v, l);
+}
+// Puts everything that reaches the floor on the list (`edges`: the row's edges too); its new length (which may exceed the room).  What reaches the floor lies in the turns
+// that reach it.  A thread whose second turn does may have more: all of its turns are read again, by everyone.
+template <typename T, int TH>
+__device__ __noinline__ int collect(const Row<T> r, int begin, int end, bool edges, const Best b, unsigned long long floor_key, TopList<TH> &l) {
+    __shared__ int s_again[TH], s_agains;
+    const float floor_v = floor_key ? key_value(floor_key) : -INFINITY;
+    const uint32_t floor_i = (uint32_t)key_index(floor_key);          // the last position that counts among equal ones
+    const int tid = threadIdx.x;
+    if (tid == 0) { l.count = 0; s_agains = 0; }
+    __syncthreads();
+    auto in = [&](float v, int w) { return v > floor_v || (v == floor_v && (uint32_t)r.index(w) <= floor_i); };
+    if (in(b.v2, b.w2)) s_again[atomicAdd(&s_agains, 1)] = begin + tid;
+    else if (in(b.v1, b.w1)) offer(r, b.w1, end, floor_key, floor_v, l);
+    if (edges && tid < Row<T>::EDGES && r.edge(tid) >= 0) {
+        const float x = to_f32(r.at(r.edge(tid)));
+        const unsigned long long key = top_key(x, r.edge(tid));
+        if (x >= floor_v && key >= floor_key) {
+            const int to = atomicAdd(&l.count, 1);
+            if (to < TopList<TH>::CAP) l.key[to] = key;
+        }
+    }
+    __syncthreads();
+    if (s_agains) {
+        const int turns = (end - begin + TH * kLpUnroll - 1) / (TH * kLpUnroll), all = s_agains * turns;
+#pragma unroll 1
+        for (int i = tid; i < all; i += TH) {
+            const int w = s_again[i / turns] + i % turns * (TH * kLpUnroll);
+            if (w < end) offer(r, w, end, floor_key, floor_v, l);
+        }
+        __syncthreads();
+    }
+    const int n = l.count;
+    __syncthreads();
+    return n;
+}
+// The k-th largest of the threads' best keys, a floor that values tied in many places do not reach (0: fewer than k threads met a number).
+template <typename T, int TH>
+__device__ __noinline__ unsigned long long exact_floor(const Row<T> r, int end, const Best b, int k, TopList<TH> &l) {
     __shared__ unsigned long long s_floor;
-    pdl_enter();
+    unsigned long long mine = 0;
+    if (b.w1 >= 0) {
+        uint4 v[kLpUnroll];
+        load_turn<T, TH>(r, b.w1, end, v, NAN);
+#pragma unroll
+        for (int u = 0; u < kLpUnroll; ++u) {
+            const unsigned long long key = word_best<T>(v[u], r.index(b.w1 + u * TH));
+            if (key > mine) mine = key;
+        }
+    }
+    l.key[threadIdx.x] = mine;
+    if (threadIdx.x == 0) s_floor = 0;
+    __syncthreads();
+    int larger = 0;
+#pragma unroll 4
+    for (int j = 0; j < TH; ++j) larger += l.key[j] > mine;
+    if (larger == k - 1 && mine) s_floor = mine;
+    __syncthreads();
+    return s_floor;
+}
+// The k best of words [begin, end) and perhaps the edges, in order, from the threads' best turns.  A floor comes first: with M = ceil(k / warps), the least of
+// the warps' M-th largest maxima; each warp has M lanes that reach it, so k values do.  Where many more do (ties: masked rows),
+// a better floor takes less time than ranking them.
+template <typename T, int TH>
+__device__ __noinline__ void top_of_words(const Row<T> r, int begin, int end, bool edges, const Best b, int k, TopList<TH> &l) {
+    __shared__ uint32_t s_least[TH / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int warps = (end - begin) / 32 < TH / 32 ? (end - begin) / 32 : TH / 32;      // whose lanes all have a word
+    const int m = warps ? (k + warps - 1) / warps : 33;
+    unsigned long long floor_key = 0;
+    if (m <= 32) {
+        uint32_t mine = b.w1 >= 0 ? order_bits(b.v1) : 0u, best = 0;
+#pragma unroll 1
+        for (int i = 0; i < m; ++i) {
+            best = __reduce_max_sync(0xffffffffu, mine);
+            const uint32_t who = __ballot_sync(0xffffffffu, mine == best);
+            if (lane == __ffs(who) - 1) mine = 0;
+        }
+        if (lane == 0) s_least[warp] = best;
+        __syncthreads();
+        best = s_least[0];
+        for (int w = 1; w < warps; ++w) best = min(best, s_least[w]);
+        floor_key = (unsigned long long)best << 32;
+    }
+    int n = 2 * TH + 1;
+    if (__syncthreads_count(b.w1 >= 0 && order_bits(b.v1) >= (uint32_t)(floor_key >> 32)) <= 2 * k + TH / 8)
+        n = collect<T, TH>(r, begin, end, edges, b, floor_key, l);
+    if (n > 2 * TH) {
+        floor_key = exact_floor<T, TH>(r, end, b, k, l);
+        n = collect<T, TH>(r, begin, end, edges, b, floor_key, l);
+    }
+    while (n > TopList<TH>::CAP) {
+        // Still more than there is room for (rows in an order made for it, rows of mostly NaN): again from the k-th best of those
+        // that had room, a floor that all but k of them no longer reach.
+        top_cut(l, TopList<TH>::CAP, k);
+        floor_key = l.key[k - 1];
+        __syncthreads();
+        n = collect<T, TH>(r, begin, end, edges, b, floor_key, l);
+    }
+    top_cut(l, n, k);
+}
+
+// What the CTAs of a cluster hand to the first: (s, m), (length of the list, w), and the list.
+template <int K> struct TopIn { unsigned long long part[8][2], key[8][K]; };
+
+template <typename T, bool TOP, int TH>
+__global__ void __launch_bounds__(TH, (TOP ? 1280 : 1536) / TH) logprobs_row_kernel(const LogprobArgs a) {
+    constexpr int VE = Row<T>::VE, U = kLpUnroll, WARPS = TH / 32;
+    __shared__ TopList<TH> s_top;
+    __shared__ Stats s_warp[WARPS];
+    __shared__ TopIn<TOP ? kTopMax : 1> s_in;
     const uint32_t rank = rows_cluster_rank(), share = rows_cluster_size();
+    if (share > 1) rows_cluster_arrive();
+    pdl_enter();
     const long long row = blockIdx.x / share;
     const Row<T> r((const T *)a.x + row * a.x_row, a.V);
     const int begin = (int)((long long)r.words * rank / share), end = (int)((long long)r.words * (rank + 1) / share);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const T fill = from_f32<T>(-INFINITY);
-    const int cut_at = kLpThreads + 2 * a.k;
 
     Stats st;
     st.reset();
-    unsigned long long floor_key = 0;            // nothing below it can be among the k best
-    float floor_v = -INFINITY;
-    if (TOP) {
-        if (threadIdx.x == 0) s_top.count = 0;
-        __syncthreads();
-    }
-    for (int w0 = begin; w0 < end; w0 += kLpThreads * U) {
-        uint4 v[U];
-        int at[U];
+    Best best;
+    best.reset();
+    auto turn = [&](const uint4 (&v)[U], int w) {
+        float top = vec_max<T>(v[0]);
+#pragma unroll
+        for (int u = 1; u < U; ++u) top = fmaxf(top, vec_max<T>(v[u]));
+        if (TOP && !(top <= best.v2)) best.see(top, w);
+        if (top > st.m) st.raise(top, a.c);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            at[u] = w0 + u * kLpThreads + (int)threadIdx.x;
-            if (at[u] < end) v[u] = r.load(at[u], fill);
-        }
-        float wmax[U], tmax = kLowest;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            wmax[u] = -INFINITY;
-            if (at[u] >= end) continue;
-            float f[VE];
-            unpack_vec<T>(v[u], f);
-#pragma unroll
-            for (int i = 0; i < VE; ++i) wmax[u] = fmaxf(wmax[u], f[i]);
-            tmax = fmaxf(tmax, wmax[u]);
-        }
-        if (tmax > st.m) st.raise(tmax, a.c);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (at[u] >= end) continue;
             float f[VE];
             unpack_vec<T>(v[u], f);
             accumulate<VE, true>(st, f, a.c);
         }
-        if (TOP) {
-            const int first_words = end - begin < kLpThreads ? end - begin : kLpThreads;
-            if (w0 == begin && first_words >= a.k) {
-                // the first tile's floor: the k-th largest of the threads' largest
-                unsigned long long best = 0;
-                if ((int)threadIdx.x < first_words) {
+    };
+    int w = begin + (int)threadIdx.x;
+    for (; w + (U - 1) * TH < end; w += TH * U) {
+        uint4 v[U];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (at[u] >= end) continue;
-                        float f[VE];
-                        unpack_vec<T>(v[u], f);
-#pragma unroll
-                        for (int i = 0; i < VE; ++i)
-                            if (r.holds((long long)at[u] * VE + i) && f[i] == f[i]) {
-                                const unsigned long long key = top_key(f[i], at[u] * VE + i - r.head);
-                                if (key > best) best = key;
-                            }
-                    }
-                }
-                s_top.key[threadIdx.x] = best;
-                __syncthreads();
-                int larger = 0;
-                for (int j = 0; j < first_words; ++j) larger += s_top.key[j] > best;
-                __syncthreads();
-                // (a key of 0: a thread that met nothing but NaN)
-                const bool kth = larger == a.k - 1 && best != 0;
-                if (kth) s_floor = best;
-                floor_key = __syncthreads_or(kth) ? s_floor : 0;
-                floor_v = floor_key ? key_value(floor_key) : -INFINITY;
-            }
-            while (true) {
-                const int floor_i = floor_key ? key_index(floor_key) : 0x7fffffff;
-                bool grown = false;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (at[u] >= end || !(wmax[u] >= floor_v)) continue;
-                    if (wmax[u] == floor_v && at[u] * VE - r.head > floor_i) continue;
-                    float f[VE];
-                    unpack_vec<T>(v[u], f);
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) {
-                        if (!(f[i] >= floor_v) || !r.holds((long long)at[u] * VE + i)) continue;
-                        const unsigned long long key = top_key(f[i], at[u] * VE + i - r.head);
-                        if (key < floor_key) continue;
-                        const int to = atomicAdd(&s_top.count, 1);
-                        if (to < kTopCap) s_top.key[to] = key;
-                        grown |= to >= cut_at;
-                    }
-                }
-                if (!__syncthreads_or(grown)) break;
-                const int n = s_top.count;
-                __syncthreads();                                   // everyone has read the count
-                top_cut(s_top, n < kTopCap ? n : kTopCap, a.k);
-                floor_key = s_top.key[a.k - 1];
-                floor_v = key_value(floor_key);
-                if (n <= kTopCap) break;
-                // Some of this tile found no room: its entries leave the list and it is walked again under the higher floor, which
-                // at least kTopCap - cut_at - k of its values no longer reach.
-                unsigned long long keep = 0;
-                if ((int)threadIdx.x < a.k) keep = s_top.key[threadIdx.x];
-                const long long pos = (long long)key_index(keep) + r.head;
-                const bool stays = keep && pos < (long long)w0 * VE;
-                __syncthreads();
-                if (threadIdx.x == 0) s_top.count = 0;
-                __syncthreads();
-                if (stays) s_top.key[atomicAdd(&s_top.count, 1)] = keep;
-                __syncthreads();
-            }
-        }
+        for (int u = 0; u < U; ++u) v[u] = r.load(w + u * TH);
+        turn(v, w);
+    }
+    if (w < end) {
+        uint4 v[U];
+        load_turn<T, TH>(r, w, end, v, -INFINITY);
+        turn(v, w);
+    }
+    if (rank == 0 && threadIdx.x < Row<T>::EDGES && r.edge(threadIdx.x) >= 0) {
+        const float x[2] = {to_f32(r.at(r.edge(threadIdx.x))), -INFINITY};
+        if (x[0] > st.m) st.raise(x[0], a.c);
+        accumulate<2, true>(st, x, a.c);
     }
     warp_join(st, a.c);
     if (lane == 0) s_warp[warp] = st;
+    if (TOP) top_of_words<T, TH>(r, begin, end, rank == 0, best, a.k, s_top);
     __syncthreads();
     if (warp == 0) {
         st.reset();
-        if (lane < kLpWarps) st = s_warp[lane];
+        if (lane < WARPS) st = s_warp[lane];
         warp_join(st, a.c);
+        __syncwarp();
         if (lane == 0) s_warp[0] = st;
+    }
+    if (share > 1) {
+        // The others' sums and lists, each in order, go to the first CTA, which merges them.
+        rows_cluster_wait();                                       // it has started
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            st_peer_u64(&s_in.part[rank][0], 0, ((unsigned long long)__float_as_uint(st.s) << 32) | __float_as_uint(st.m));
+            st_peer_u64(&s_in.part[rank][1], 0, ((unsigned long long)(TOP ? s_top.count : 0) << 32) | __float_as_uint(st.w));
+        }
+        if (TOP && (int)threadIdx.x < s_top.count) st_peer_u64(&s_in.key[rank][threadIdx.x], 0, s_top.key[threadIdx.x]);
+        rows_cluster_sync();
+        if (rank != 0) return;
+        if (warp == 0) {
+            st.reset();
+            if (lane < (int)share) {
+                st.m = __uint_as_float((uint32_t)s_in.part[lane][0]);
+                st.s = __uint_as_float((uint32_t)(s_in.part[lane][0] >> 32));
+                st.w = __uint_as_float((uint32_t)s_in.part[lane][1]);
+            }
+            warp_join(st, a.c);
+            if (lane == 0) s_warp[0] = st;
+        }
+        if (TOP) {
+            for (int i = threadIdx.x; i < (int)share * a.k; i += TH) {
+                const int list = i / a.k, j = i - list * a.k;
+                if (j >= (int)(s_in.part[list][1] >> 32)) continue;
+                const unsigned long long mine = s_in.key[list][j];
+                int ahead = j;
+                for (int o = 0; o < (int)share && ahead < a.k; ++o) {
+                    if (o == list) continue;
+                    int low = 0, high = (int)(s_in.part[o][1] >> 32);         // the number of larger keys
+                    while (low < high) {
+                        const int mid = (low + high) >> 1;
+                        if (s_in.key[o][mid] > mine) low = mid + 1;
+                        else high = mid;
+                    }
+                    ahead += low;
+                }
+                if (ahead < a.k) s_top.key[ahead] = mine;
+            }
+            if (threadIdx.x == 0) {
+                int n = 0;
+                for (int o = 0; o < (int)share; ++o) n += (int)(s_in.part[o][1] >> 32);
+                s_top.count = n < a.k ? n : a.k;
+            }
+        }
+    }
+    __shared__ RowAnswer s_answer;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const RowAnswer ans(s_warp[0], a.inv_t);
+        s_answer = ans;
+        answer_row<T>(a, row, s_warp[0], ans);
     }
     if (TOP) {
         __syncthreads();
-        const int n = s_top.count;
-        __syncthreads();
-        top_cut(s_top, n, a.k);
-    }
-    if (share > 1) {
-        __shared__ unsigned long long s_part[2];
-        if (threadIdx.x == 0) {
-            s_part[0] = ((unsigned long long)__float_as_uint(s_warp[0].s) << 32) | __float_as_uint(s_warp[0].m);
-            s_part[1] = ((unsigned long long)(TOP ? s_top.count : 0) << 32) | __float_as_uint(s_warp[0].w);
+        if ((int)threadIdx.x < a.k) {
+            const bool have = (int)threadIdx.x < s_top.count;
+            const unsigned long long key = have ? s_top.key[threadIdx.x] : 0;
+            a.top_logprob[row * a.k + threadIdx.x] = have ? s_answer.of(key_value(key)) : NAN;
+            a.top_index[row * a.k + threadIdx.x] = have ? key_index(key) : -1;
         }
-        __syncthreads();
-        rows_cluster_sync();
-        if (rank == 0) {
-            int n = TOP ? s_top.count : 0;
-            __syncthreads();                                       // before the list grows
-            Stats all = s_warp[0];
-            for (uint32_t o = 1; o < share; ++o) {
-                const unsigned long long p0 = ld_peer_u64(&s_part[0], o), p1 = ld_peer_u64(&s_part[1], o);
-                Stats b;
-                b.m = __uint_as_float((uint32_t)p0);
-                b.s = __uint_as_float((uint32_t)(p0 >> 32));
-                b.w = __uint_as_float((uint32_t)p1);
-                all.join(b, a.c);
-                if (TOP) {
-                    const int more = (int)(p1 >> 32);
-                    if ((int)threadIdx.x < more) s_top.key[n + threadIdx.x] = ld_peer_u64(&s_top.key[threadIdx.x], o);
-                    n += more;
-                }
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) s_warp[0] = all;
-            if (TOP) top_cut(s_top, n, a.k);
-        }
-        __syncthreads();
-        rows_cluster_sync();                                       // no CTA leaves while its shared memory is read
-        if (rank != 0) return;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) answer_row<T>(a, row, s_warp[0]);
-    if (TOP && (int)threadIdx.x < a.k) {
-        const RowAnswer ans(s_warp[0], a.inv_t);
-        const bool have = (int)threadIdx.x < s_top.count;
-        const unsigned long long key = have ? s_top.key[threadIdx.x] : 0;
-        a.top_logprob[row * a.k + threadIdx.x] = have ? ans.of(key_value(key)) : NAN;
-        a.top_index[row * a.k + threadIdx.x] = have ? key_index(key) : -1;
     }
 }
 
@@ -275,9 +394,9 @@ __global__ void __launch_bounds__(128) logprobs_warp_kernel(const LogprobArgs a)
     st.raise(m, a.c);
     accumulate<E, true>(st, f, a.c);
     warp_join(st, a.c);
-    if (lane == 0) answer_row<T>(a, row, st);
-    if (a.k == 0) return;
     const RowAnswer ans(st, a.inv_t);
+    if (lane == 0) answer_row<T>(a, row, st, ans);
+    if (a.k == 0) return;
     uint32_t taken = 0;
     for (int j = 0; j < a.k; ++j) {
         uint32_t best = 0;                       // order bits of a number are never 0 (that is a NaN's)
@@ -319,39 +438,38 @@ __global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogprobBwdArgs 
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (w0 + u * 32 < r.words) v[u] = r.load(w0 + u * 32, from_f32<T>(0.f));
+        if (w0 + u * 32 < r.words) v[u] = r.load(w0 + u * 32);
     const int t = a.tokens ? a.tokens[row] : -1;
     const bool some = t >= 0 && t < a.V;
     const float lse = a.lse[row], g = a.g_logprob && some ? a.g_logprob[row] : 0.f;
     const float h = a.g_entropy ? a.g_entropy[row] : 0.f, l = a.g_lse ? a.g_lse[row] : 0.f;
     const float base = l - g - (a.g_entropy ? h * a.entropy[row] : 0.f);
     const bool none = lse < -1e30f;              // nothing but mask values: no gradient
-    const bool same = (((uintptr_t)dx & 15) / sizeof(T)) == (uintptr_t)r.head;
+    auto grad = [&](float x, int index) {
+        const float lp = max_nan(fmaf(x, a.inv_t, -lse), kFar), p = ex2(lp * kLog2e);
+        float d = p * fmaf(-h, lp, base);
+        if (none) d = 0.f;
+        else if (index == t) d += g;
+        return d * a.inv_t;
+    };
+    const bool same = ((uintptr_t)(dx + r.head) & 15) == 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int w = w0 + u * 32;
         if (w >= r.words) continue;
         float f[VE];
         unpack_vec<T>(v[u], f);
-        const int first = w * VE - r.head;
+        const int first = r.index(w);
 #pragma unroll
-        for (int i = 0; i < VE; ++i) {
-            const float lp = max_nan(fmaf(f[i], a.inv_t, -lse), kFar), p = ex2(lp * kLog2e);
-            float d = p * fmaf(-h, lp, base);
-            if (none) d = 0.f;
-            if (first + i == t && !none) d += g;
-            f[i] = d * a.inv_t;
-        }
-        if (same && r.whole(w)) {
-            constexpr int PER = 4 / (int)sizeof(T);
-            *reinterpret_cast<uint4 *>(dx + first) =
-                make_uint4(pack_word(f, T()), pack_word(f + PER, T()), pack_word(f + 2 * PER, T()), pack_word(f + 3 * PER, T()));
-        } else {
+        for (int i = 0; i < VE; ++i) f[i] = grad(f[i], first + i);
+        if (same) *reinterpret_cast<uint4 *>(dx + first) = pack_vec<T>(f);
+        else {
 #pragma unroll
-            for (int i = 0; i < VE; ++i)
-                if (r.holds((long long)w * VE + i)) dx[first + i] = from_f32<T>(f[i]);
+            for (int i = 0; i < VE; ++i) dx[first + i] = from_f32<T>(f[i]);
         }
     }
+    if (item == row * a.chunks && lane < Row<T>::EDGES && r.edge(lane) >= 0)
+        dx[r.edge(lane)] = from_f32<T>(grad(to_f32(r.at(r.edge(lane))), r.edge(lane)));
 }
 
 }  // namespace lpdt
@@ -383,7 +501,11 @@ extern "C" lpdt_status lpdt_token_logprobs(int64_t rows, int32_t V, const void *
             else launch_k(logprobs_warp_kernel<T, 32>, grid, 128, 0, st, a);
         } else {
             const int cs = row_share(rows, (int64_t)V * sizeof(T), 4, 4096);
-            launch_k_cluster(top_k ? logprobs_row_kernel<T, true> : logprobs_row_kernel<T, false>, (unsigned)(rows * cs), kLpThreads, 0, st, cs, a);
+            const unsigned grid = (unsigned)(rows * cs);
+            if ((int64_t)V * (int64_t)sizeof(T) / cs <= 16384)
+                launch_k_cluster(top_k ? logprobs_row_kernel<T, true, 128> : logprobs_row_kernel<T, false, 128>, grid, 128, 0, st, cs, a);
+            else
+                launch_k_cluster(top_k ? logprobs_row_kernel<T, true, 256> : logprobs_row_kernel<T, false, 256>, grid, 256, 0, st, cs, a);
         }
         LPDT_LAUNCH_CHECK();
         return LPDT_OK;
@@ -410,7 +532,7 @@ extern "C" lpdt_status lpdt_token_logprobs_bwd(int64_t rows, int32_t V, const vo
     return with_dtype(dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
         constexpr int VE = Row<T>::VE;
-        a.chunks = (int)ceil_div((int64_t)V + VE - 1, 128 * VE);
+        a.chunks = (int)ceil_div(V, 128 * VE);
         const int64_t blocks = ceil_div(rows * a.chunks, 8);
         if (blocks > 0x7fffffff) return LPDT_ERR_UNSUPPORTED;
         launch_k(logprobs_bwd_kernel<T>, (unsigned)blocks, 256, 0, st, a);
