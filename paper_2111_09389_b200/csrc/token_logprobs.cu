@@ -134,19 +134,27 @@ __device__ __noinline__ void word_offer(uint4 v, int index, unsigned long long f
         if (to < TopList<TH>::CAP) l.key[to] = key;
     }
 }
-// A thread's turn from word w on; what is not there is `fill`.
+// A thread takes its words in turns of kLpUnroll, TH apart, and the last few one by one.  The words of the turn from w on; those of no turn
+// are NaN.
 template <typename T, int TH>
-__device__ __forceinline__ void load_turn(const Row<T> &r, int w, int end, uint4 (&v)[kLpUnroll], float fill) {
+__device__ __forceinline__ void load_turn(const Row<T> &r, int w, int end, uint4 (&v)[kLpUnroll]) {
+    const bool full = w + (kLpUnroll - 1) * TH < end;
+    v[0] = r.load(w);
 #pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u) v[u] = w + u * TH < end ? r.load(w + u * TH) : same_word(from_f32<T>(fill));
+    for (int u = 1; u < kLpUnroll; ++u) v[u] = full ? r.load(w + u * TH) : same_word(from_f32<T>(NAN));
 }
 template <typename T, int TH>
 __device__ __forceinline__ void offer(const Row<T> &r, int w, int end, unsigned long long floor_key, float floor_v, TopList<TH> &l) {
     uint4 v[kLpUnroll];
-    load_turn<T, TH>(r, w, end, v, NAN);
+    load_turn<T, TH>(r, w, end, v);
+    uint32_t in = 0;
 #pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u)
-        if (vec_max<T>(v[u]) >= floor_v) word_offer<T, TH>(v[u], r.index(w + u * TH), floor_key, floor_v, l);
+    for (int u = 0; u < kLpUnroll; ++u) in |= (uint32_t)(vec_max<T>(v[u]) >= floor_v) << u;
+    for (; in; in &= in - 1) {                   // one word, as a rule: one call for the warp's lanes
+        const int u = __ffs(in) - 1;
+        const uint4 x = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
+        word_offer<T, TH>(x, r.index(w + u * TH), floor_key, floor_v, l);
+    }
 }
 // Puts everything that reaches the floor on the list (`edges`: the row's edges too); its new length (which may exceed the room).  What reaches the floor lies in the turns
 // that reach it.  A thread whose second turn does may have more: all of its turns are read again, by everyone.
@@ -171,10 +179,12 @@ __device__ __noinline__ int collect(const Row<T> r, int begin, int end, bool edg
     }
     __syncthreads();
     if (s_agains) {
-        const int turns = (end - begin + TH * kLpUnroll - 1) / (TH * kLpUnroll), all = s_agains * turns;
+        const int full = (end - begin) / (TH * kLpUnroll), turns = full + kLpUnroll, all = s_agains * turns;      // each thread's, at most
 #pragma unroll 1
         for (int i = tid; i < all; i += TH) {
-            const int w = s_again[i / turns] + i % turns * (TH * kLpUnroll);
+            const int t = i % turns, first = s_again[i / turns];
+            const int own = end - first < TH * (kLpUnroll - 1) + 1 ? 0 : (end - first - TH * (kLpUnroll - 1) - 1) / (TH * kLpUnroll) + 1;
+            const int w = first + (t < own ? t * kLpUnroll : own * kLpUnroll + t - own) * TH;
             if (w < end) offer(r, w, end, floor_key, floor_v, l);
         }
         __syncthreads();
@@ -190,7 +200,7 @@ __device__ __noinline__ unsigned long long exact_floor(const Row<T> r, int end, 
     unsigned long long mine = 0;
     if (b.w1 >= 0) {
         uint4 v[kLpUnroll];
-        load_turn<T, TH>(r, b.w1, end, v, NAN);
+        load_turn<T, TH>(r, b.w1, end, v);
 #pragma unroll
         for (int u = 0; u < kLpUnroll; ++u) {
             const unsigned long long key = word_best<T>(v[u], r.index(b.w1 + u * TH));
@@ -270,7 +280,11 @@ __global__ void __launch_bounds__(TH, (TOP ? 1280 : 1536) / TH) logprobs_row_ker
     st.reset();
     Best best;
     best.reset();
-    auto turn = [&](const uint4 (&v)[U], int w) {
+    int w = begin + (int)threadIdx.x;
+    for (; w + (U - 1) * TH < end; w += TH * U) {
+        uint4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = r.load(w + u * TH);
         float top = vec_max<T>(v[0]);
 #pragma unroll
         for (int u = 1; u < U; ++u) top = fmaxf(top, vec_max<T>(v[u]));
@@ -282,18 +296,15 @@ __global__ void __launch_bounds__(TH, (TOP ? 1280 : 1536) / TH) logprobs_row_ker
             unpack_vec<T>(v[u], f);
             accumulate<VE, true>(st, f, a.c);
         }
-    };
-    int w = begin + (int)threadIdx.x;
-    for (; w + (U - 1) * TH < end; w += TH * U) {
-        uint4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = r.load(w + u * TH);
-        turn(v, w);
     }
-    if (w < end) {
-        uint4 v[U];
-        load_turn<T, TH>(r, w, end, v, -INFINITY);
-        turn(v, w);
+    for (; w < end; w += TH) {
+        const uint4 v = r.load(w);
+        const float top = vec_max<T>(v);
+        if (TOP && !(top <= best.v2)) best.see(top, w);
+        if (top > st.m) st.raise(top, a.c);
+        float f[VE];
+        unpack_vec<T>(v, f);
+        accumulate<VE, true>(st, f, a.c);
     }
     if (rank == 0 && threadIdx.x < Row<T>::EDGES && r.edge(threadIdx.x) >= 0) {
         const float x[2] = {to_f32(r.at(r.edge(threadIdx.x))), -INFINITY};
