@@ -23,7 +23,7 @@
 namespace lpdt {
 namespace tc {
 
-constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleBytes = 1536, kMmMaxRows = 240 /*2 * 240 + 32 <= 512*/, kMmRaster = 8;
+constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleBytes = 1536, kMmScaleSlots = 4, kMmMaxRows = 240 /*2 * 240 + 32 <= 512*/, kMmRaster = 8;
 constexpr size_t kMmSmem = 227 * 1024;
 
 struct MmParams {
@@ -38,7 +38,7 @@ struct MmParams {
     int32_t *dev_status;
 };
 struct MmCtl {
-    unsigned long long full[kMmMaxStages], empty[kMmMaxStages], tmem_full[2], tmem_empty[2];
+    unsigned long long full[kMmMaxStages], empty[kMmMaxStages], sf_full[kMmScaleSlots], sf_done[kMmScaleSlots], tmem_full[2], tmem_empty[2];
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -93,8 +93,10 @@ template <int G> __device__ __forceinline__ void mm_commit(uint32_t bar) {
     else
         mma_commit(bar);
 }
-// kind::mxf8f6f4, e4m3 operands (both K-major), UE8M0 scale factors in byte 0 of their words, M lanes x N columns.
-__host__ __device__ constexpr uint32_t idesc_mx_e4m3(int M, int N) { return ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27); }
+// kind::mxf8f6f4, e4m3 operands (both K-major), UE8M0 scale factors in byte `sf` of their words, M lanes x N columns.
+__host__ __device__ constexpr uint32_t idesc_mx_e4m3(int M, int N, uint32_t sf = 0) {
+    return (sf << 4) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 7) << 27) | (sf << 29);
+}
 
 struct MmTile { int node, jt, mt; };
 // Groups of kMmRaster column tiles sweep all row tiles, so that the tiles in flight share operand panels in L2.
@@ -156,7 +158,8 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     const int halfn = p.bn / G;                                         // rows of A per CTA
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1 + G); mbar_init(smem_u32(&ctl->empty[i]), 1); }
+        for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
+        for (int i = 0; i < kMmScaleSlots; ++i) { mbar_init(smem_u32(&ctl->sf_full[i]), G); mbar_init(smem_u32(&ctl->sf_done[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->tmem_full[i]), 1); mbar_init(smem_u32(&ctl->tmem_empty[i]), 8 * G); }
         ctl->abort_flag = 0;
         mbar_fence_init();
@@ -206,41 +209,54 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             const uint32_t idesc = idesc_mx_e4m3(128 * G, p.bn);
             const uint64_t tpl = smem_desc(0, 16, 1024, 2), sc_tpl = smem_desc(0, 16, 128, 0);
             const uint32_t sf0 = tmem_base + 2 * p.bn;
-            int st = 0; uint32_t ph = 0, tcount = 0, sfset = 0;
+            int st = 0; uint32_t ph = 0, tcount = 0, group = 0;
             for (int tile = first; tile < total && !ctl->abort_flag; tile += step, ++tcount) {
                 const int acc = tcount & 1;
                 if (!mbar_wait(smem_u32(&ctl->tmem_empty[acc]), ((tcount >> 1) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) break;
                 tc_fence_after();
                 bool ok = true;
                 for (int kb = k_begin; kb < k_end; ++kb) {
+                    if (kb == k_begin || (kb & 3) == 0) {
+                        // The next four blocks' factors, into the set of columns that the group before last has left: its products are
+                        // done (those of the last group keep the tensor cores busy meanwhile).
+                        const int slot = group & (kMmScaleSlots - 1), old = (group - 2) & (kMmScaleSlots - 1);
+                        if (group >= 2 && !mbar_wait(smem_u32(&ctl->sf_done[old]), ((group - 2) / kMmScaleSlots) & 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
+                        if (!mbar_wait(smem_u32(&ctl->sf_full[slot]), (group / kMmScaleSlots) & 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t sc = smem_u32(scales + (size_t)slot * kMmScaleBytes) >> 4, sf = sf0 + (group & 1) * 16;
+                            mm_copy_scales<G>(sf, sc_tpl | (sc & 0x3FFFu));
+                            mm_copy_scales<G>(sf + 4, sc_tpl | ((sc + 32) & 0x3FFFu));
+                            if (p.bn > 128) mm_copy_scales<G>(sf + 8, sc_tpl | ((sc + 64) & 0x3FFFu));
+                        }
+                        __syncwarp();
+                        ++group;
+                    }
                     if (!mbar_wait(smem_u32(&ctl->full[st]), ph, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint32_t sc = smem_u32(scales + (size_t)st * kMmScaleBytes) >> 4, sf = sf0 + (sfset & 1) * 16;
-                        mm_copy_scales<G>(sf, sc_tpl | (sc & 0x3FFFu));
-                        mm_copy_scales<G>(sf + 4, sc_tpl | ((sc + 32) & 0x3FFFu));
-                        if (p.bn > 128) mm_copy_scales<G>(sf + 8, sc_tpl | ((sc + 64) & 0x3FFFu));
+                        const uint32_t id = idesc | ((uint32_t)(kb & 3) << 4) | ((uint32_t)(kb & 3) << 29), sf = sf0 + ((group - 1) & 1) * 16;
                         uint32_t l = smem_u32(data + (size_t)st * p.slot) >> 4, r = l + (kMmLaneBytes >> 4);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            mm_mma<G>(tmem_base + acc * p.bn, tpl | (l & 0x3FFFu), tpl | (r & 0x3FFFu), idesc, sf, sf + 4, (uint32_t)((kb - k_begin) | k));
+                            mm_mma<G>(tmem_base + acc * p.bn, tpl | (l & 0x3FFFu), tpl | (r & 0x3FFFu), id, sf, sf + 4, (uint32_t)((kb - k_begin) | k));
                             l += 2; r += 2;
                         }
                         mm_commit<G>(smem_u32(&ctl->empty[st]));
+                        if ((kb & 3) == 3 || kb == k_end - 1) mm_commit<G>(smem_u32(&ctl->sf_done[(group - 1) & (kMmScaleSlots - 1)]));
                         if (kb == k_end - 1) mm_commit<G>(smem_u32(&ctl->tmem_full[acc]));
                     }
                     __syncwarp();
-                    ++sfset;
                     if (++st == p.stages) { st = 0; ph ^= 1; }
                 }
                 if (!ok) break;
             }
         }
     } else if (warp == 2) {
-        // Row r of a group of 128 goes to bytes (r % 32) * 16 + (r / 32) * 4 on; each word holds the block's scale four times.  Of a row's
-        // scales four blocks lie in a word: one load per row and four stages, the next group's issued before this one's are used.
-        const int groups = p.bn > 128 ? 3 : 2;
-        int st = 0; uint32_t ph = 0;
+        // Row r of 128 goes to bytes (r % 32) * 16 + (r / 32) * 4 on: the word that holds its scales of four blocks of K (the instruction
+        // names the byte).  The next words are on their way while this group waits for its slot.
+        const int sets = p.bn > 128 ? 3 : 2;
+        uint32_t group = 0;
         for (int tile = first; tile < total && !ctl->abort_flag; tile += step) {
             const MmTile t = mm_tile(p, tile);
             const int j0 = (t.jt * G + (G == 2 ? (int)rank : 0)) * 128, m0 = t.mt * p.bn;
@@ -255,35 +271,34 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             auto fetch = [&](int word) {
 #pragma unroll
                 for (int i = 0; i < 12; ++i)
-                    next[i] = (i < 8 || groups == 3) && row[i] ? __ldg(reinterpret_cast<const uint32_t *>(row[i]) + word) : 0x7f7f7f7fu;
+                    next[i] = (i < 8 || sets == 3) && row[i] ? __ldg(reinterpret_cast<const uint32_t *>(row[i]) + word) : 0x7f7f7f7fu;
             };
+            const int last = (k_end - 1) >> 2;
             fetch(k_begin >> 2);
-            uint32_t now[12];
             bool ok = true;
-            for (int kb = k_begin; kb < k_end; ++kb) {
-                if (kb == k_begin || (kb & 3) == 0) {
+            for (int g = k_begin >> 2; g <= last; ++g, ++group) {
+                const int slot = group & (kMmScaleSlots - 1);
+                uint32_t now[12];
 #pragma unroll
-                    for (int i = 0; i < 12; ++i) now[i] = next[i];
-                    if ((kb >> 2) < ((k_end - 1) >> 2)) fetch((kb >> 2) + 1);
-                }
-                if (!mbar_wait(smem_u32(&ctl->empty[st]), ph ^ 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
-                const uint32_t sel = 0x1111u * (uint32_t)(kb & 3);
-                uint4 *dst = reinterpret_cast<uint4 *>(scales + (size_t)st * kMmScaleBytes) + lane;
+                for (int i = 0; i < 12; ++i) now[i] = next[i];
+                if (g < last) fetch(g + 1);
+                if (!mbar_wait(smem_u32(&ctl->sf_done[slot]), ((group / kMmScaleSlots) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
+                uint4 *dst = reinterpret_cast<uint4 *>(scales + (size_t)slot * kMmScaleBytes) + lane;
 #pragma unroll
-                for (int g = 0; g < 3; ++g)
-                    if (g < groups)
-                        dst[g * 32] = make_uint4(__byte_perm(now[4 * g], 0, sel), __byte_perm(now[4 * g + 1], 0, sel),
-                                                 __byte_perm(now[4 * g + 2], 0, sel), __byte_perm(now[4 * g + 3], 0, sel));
+                for (int i = 0; i < 3; ++i)
+                    if (i < sets) dst[i * 32] = make_uint4(now[4 * i], now[4 * i + 1], now[4 * i + 2], now[4 * i + 3]);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if (G == 2) mm_arrive_at(mm_peer(smem_u32(&ctl->full[st]), 0));
-                    else mbar_arrive(smem_u32(&ctl->full[st]));
+                    if (G == 2) mm_arrive_at(mm_peer(smem_u32(&ctl->sf_full[slot]), 0));
+                    else mbar_arrive(smem_u32(&ctl->sf_full[slot]));
                 }
-                if (++st == p.stages) { st = 0; ph ^= 1; }
             }
             if (!ok) break;
         }
+        // (commits reach these barriers like the empty ones)
+        for (int i = 0; i < kMmScaleSlots && !ctl->abort_flag; ++i, ++group)
+            mbar_wait(smem_u32(&ctl->sf_done[group & (kMmScaleSlots - 1)]), ((group / kMmScaleSlots) & 1) ^ 1, &ctl->abort_flag, p.dev_status);
     } else if (warp >= 4) {
         const int q = warp & 3, half = (warp - 4) >> 2, chunks = p.bn / 16;
         const uint32_t empty0 = G == 2 ? mm_peer(smem_u32(&ctl->tmem_empty[0]), 0) : smem_u32(&ctl->tmem_empty[0]);
@@ -444,7 +459,7 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     const int64_t tiles = (int64_t)nodes * p.tilesJ * p.tilesM;
     if (tiles > 0x3fffffff) return LPDT_ERR_UNSUPPORTED;
     p.slot = kMmLaneBytes + (int)align_up((size_t)(plan.bn / plan.g) * 128, 1024);
-    p.stages = (int)((kMmSmem - 1024) / (p.slot + kMmScaleBytes));
+    p.stages = (int)((kMmSmem - 1024 - kMmScaleSlots * kMmScaleBytes) / p.slot);
     if (p.stages > kMmMaxStages) p.stages = kMmMaxStages;
     for (p.tmem_cols = 64; p.tmem_cols < 2 * plan.bn + 32; p.tmem_cols *= 2) {}
     p.sA = sA; p.sB = sB; p.spitch = (int)lpdt_e4m3_scale_pitch(K);
@@ -458,7 +473,7 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     const uint32_t bL[3] = {128, 128, 1}, bR[3] = {128, (uint32_t)(plan.bn / plan.g), 1};
     if (!make_map_u8(&mL, B, 3, dL, sL, bL, CU_TENSOR_MAP_SWIZZLE_128B) || !make_map_u8(&mR, A, 3, dR, sR, bR, CU_TENSOR_MAP_SWIZZLE_128B))
         return LPDT_ERR_CUDA;
-    const size_t smem = 1024 + (size_t)p.stages * (p.slot + kMmScaleBytes);
+    const size_t smem = 1024 + (size_t)p.stages * p.slot + kMmScaleSlots * kMmScaleBytes;
     const cudaStream_t st = as_stream(stream);
     return with_dtype(c_dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
