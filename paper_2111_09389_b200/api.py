@@ -94,6 +94,11 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
+def _stream_handle():
+    """The same without a Stream object, which takes 3 us to make: for calls that are often made by themselves."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _host(a):
     """Address of a host array for the duration of the call (a recording keeps the array for its replays)."""
     if _recording.calls is not None:
@@ -280,7 +285,7 @@ def lpdt_quantize_e4m3(x, nodes, rows, cols, q=None, scale=None, qt=None, scale_
     xr = cols if x_row_stride is None else x_row_stride
     xn = rows * xr if x_node_stride is None else x_node_stride
     _check("lpdt_quantize_e4m3", lib().lpdt_quantize_e4m3(_ptr(x), _dtype(x), nodes, rows, cols, xn, xr, _ptr(q), _ptr(scale),
-                                                          _ptr(qt), _ptr(scale_t), _stream()))
+                                                          _ptr(qt), _ptr(scale_t), _stream_handle()))
 
 
 def lpdt_matmul_e4m3(nodes, M, N, K, A, sA, B, sB, C, bias=None, bias_node_stride=0, addend=None, c_row_stride=None,
@@ -291,7 +296,7 @@ def lpdt_matmul_e4m3(nodes, M, N, K, A, sA, B, sB, C, bias=None, bias_node_strid
     assert addend is None or addend.dtype == C.dtype, "addend has the type of C"
     _check("lpdt_matmul_e4m3", lib().lpdt_matmul_e4m3(
         nodes, M, N, K, _ptr(A), _ptr(sA), _ptr(B), _ptr(sB), _ptr(bias), bias_node_stride, _ptr(addend), _ptr(C), _dtype(C),
-        cn, cr, _ptr(dev_status), _stream()))
+        cn, cr, _ptr(dev_status), _stream_handle()))
 
 
 def lpdt_range_evonorm_fwd(nodes, B, H, W, Cc, groups, eps, x, v, gamma, beta, param_node_stride, y,
@@ -524,7 +529,7 @@ def lpdt_token_logprobs(rows, V, logits, tokens=None, logprob=None, entropy=None
     """logits fp32, bf16 or fp16 [rows][V]; tokens, top_index int32; the rest fp32."""
     _check("lpdt_token_logprobs", lib().lpdt_token_logprobs(
         rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _ptr(tokens), _ptr(logprob),
-        _ptr(entropy), _ptr(lse), top_k, _ptr(top_logprob), _ptr(top_index), _ptr(dev_status), _stream()))
+        _ptr(entropy), _ptr(lse), top_k, _ptr(top_logprob), _ptr(top_index), _ptr(dev_status), _stream_handle()))
 
 
 def lpdt_token_logprobs_bwd(rows, V, logits, tokens, lse, entropy, dlogits, d_logprob=None, d_entropy=None, d_lse=None,
@@ -534,7 +539,7 @@ def lpdt_token_logprobs_bwd(rows, V, logits, tokens, lse, entropy, dlogits, d_lo
     _check("lpdt_token_logprobs_bwd", lib().lpdt_token_logprobs_bwd(
         rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _ptr(tokens), _ptr(lse),
         _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(d_lse), _ptr(dlogits),
-        V if dlogits_row_stride is None else dlogits_row_stride, _stream()))
+        V if dlogits_row_stride is None else dlogits_row_stride, _stream_handle()))
 
 
 def lpdt_distill_topk(nodes, B, V, logits, k, teacher_logprob, teacher_index, loss, row_loss, dlogits=None, row_weight=None,
@@ -544,7 +549,7 @@ def lpdt_distill_topk(nodes, B, V, logits, k, teacher_logprob, teacher_index, lo
     _check("lpdt_distill_topk", lib().lpdt_distill_topk(
         nodes, B, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, k, _ptr(teacher_logprob),
         _ptr(teacher_index), int(tail), _ptr(row_weight), _ptr(loss), _ptr(row_loss), _ptr(dlogits),
-        V if dlogits_row_stride is None else dlogits_row_stride, _ptr(dev_status), _stream()))
+        V if dlogits_row_stride is None else dlogits_row_stride, _ptr(dev_status), _stream_handle()))
 
 
 def lpdt_colsum(nodes, B, Cc, x, out, out_node_stride):

@@ -7,11 +7,12 @@
 // pass is one exponential and one product a value, and the listed tokens' gradients are written over it.
 //
 // Memory is the bound: the row once in, the gradient once out.
+#include <type_traits>
 #include "rows.cuh"
 
 namespace lpdt {
 
-constexpr int kDtThreads = 256, kDtWarps = kDtThreads / 32, kDtUnroll = 4, kListMax = 128;
+constexpr int kDtUnroll = 4, kListMax = 128;
 constexpr size_t kDtSmem = 160 * 1024;
 
 struct DistillArgs {
@@ -26,28 +27,56 @@ struct DistillArgs {
     int32_t *dev_status;
 };
 
-// A row's list, ready for use: in shared memory.
-struct List {
-    int id[kListMax];                 // -1: no entry
-    float x[kListMax];                // the student's logit
-    double t[kListMax], logt[kListMax];
+// A row's list in shared memory.
+template <int K> struct List {
+    double t[K], logt[K];
     double sum;                       // of t
-    double lse;                       // of the listed tokens' z, each token once; -inf without any
-    int first[kListMax];              // the entry is the first one of its token
+    float x[K];                       // the student's logit
+    int id[K];                        // -1: no entry
 };
-
-// By all threads of a warp.
 __device__ __forceinline__ double warp_max_d(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
-// Fills the list of a row; one warp, which may not use it before a barrier of its readers.
-template <typename T>
-__device__ __forceinline__ void make_list(const DistillArgs &a, long long row, List &l, int lane, bool report) {
+// Makes the teacher's probabilities of a list whose logt are what it says (-inf: no entry): one warp, entries lane, lane + 32, ...
+template <int K>
+__device__ __forceinline__ void finish_list(const DistillArgs &a, List<K> &l, int lane) {
+    constexpr int PER = K / 32;
+    double logt[PER], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        logt[i] = lane + 32 * i < a.k ? l.logt[lane + 32 * i] : -INFINITY;
+        top = fmax(top, logt[i]);
+    }
+    double shift = 0.0;
+    if (!a.tail) {
+        // the list as a distribution: minus the logarithm of its sum (a list of nothing but -inf stays as it is)
+        top = warp_max_d(top);
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (logt[i] > -INFINITY) sum += exp(logt[i] - top);
+        sum = warp_sum(sum);
+        if (top > -INFINITY) shift = top + log(sum);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int j = lane + 32 * i;
+        if (j >= a.k) continue;
+        l.logt[j] = logt[i] - shift;
+        l.t[j] = exp(logt[i] - shift);
+        sum += l.t[j];
+    }
+    sum = warp_sum(sum);
+    if (lane == 0) l.sum = sum;
+    __syncwarp();
+}
+// Reads the list of a row first.
+template <typename T, int K>
+__device__ __forceinline__ void make_list(const DistillArgs &a, long long row, List<K> &l, int lane, bool report) {
     const T *x = (const T *)a.x + row * a.x_row;
-    double top = -INFINITY, xmax = -INFINITY;
-    bool bad = false;
     for (int j = lane; j < a.k; j += 32) {
         const int id = a.index[row * a.k + j];
         const bool have = id >= 0 && id < a.V;
@@ -55,122 +84,127 @@ __device__ __forceinline__ void make_list(const DistillArgs &a, long long row, L
         l.id[j] = have ? id : -1;
         l.x[j] = have ? to_f32(x[id]) : -INFINITY;
         l.logt[j] = have ? (double)a.value[row * a.k + j] : -INFINITY;
-        top = fmax(top, l.logt[j]);
-        xmax = fmax(xmax, (double)l.x[j]);
-        bad |= l.x[j] != l.x[j];
     }
     __syncwarp();
-    double sum = 0.0, sumx = 0.0;
-    if (!a.tail) {
-        // the list as a distribution: minus the logarithm of its sum
-        top = warp_max_d(top);
-        for (int j = lane; j < a.k; j += 32)
-            if (l.logt[j] > -INFINITY) sum += exp(l.logt[j] - top);
-        const double norm = top + log(warp_sum(sum));
-        sum = 0.0;
-        for (int j = lane; j < a.k; j += 32)
-            if (l.id[j] >= 0 && l.logt[j] > -INFINITY) l.logt[j] -= norm;
-    }
-    xmax = warp_max_d(xmax);
-    const bool some = xmax > -INFINITY;
-    bad = __any_sync(0xffffffffu, bad);
-    for (int j = lane; j < a.k; j += 32) {
-        const int id = l.id[j];
-        l.t[j] = id >= 0 ? exp(l.logt[j]) : 0.0;
-        sum += l.t[j];
-        bool first = id >= 0;
-        for (int i = 0; i < j && first; ++i) first = l.id[i] != id;
-        l.first[j] = first;
-        if (first && some) sumx += exp(((double)l.x[j] - xmax) * a.inv_t);
-    }
-    sum = warp_sum(sum);
-    sumx = warp_sum(sumx);
-    if (lane == 0) {
-        l.sum = sum;
-        l.lse = bad ? NAN : some ? xmax * a.inv_t + log(sumx) : -INFINITY;
-    }
-    __syncwarp();
+    finish_list(a, l, lane);
 }
 
-// What the row's gradient and loss come from, once the sums outside the list are known.  One warp; results in all of its lanes.
-// left: the teacher's mass outside the list; rest: the factor of 2^((x - m) c) there.  A student's row of nothing but mask values
-// (lse below -1e30) has neither loss nor gradient.
-struct RowTerms { double loss, lse, left; float rest; bool masked; };
-__device__ __forceinline__ double log_add(double a, double b) {
-    if (a != a || b != b) return NAN;
-    const double m = fmax(a, b);
-    if (m == -INFINITY) return m;
-    return m + log(exp(a - m) + exp(b - m));
-}
-__device__ __forceinline__ RowTerms row_terms(const DistillArgs &a, const List &l, const Stats &st, double g, int lane) {
+// What a row's gradient comes from once the sums are known: st over the tokens outside the list, sl over those on it, each once.  Only
+// sums and quotients: m is the larger maximum, all the sum relative to it.  left: the teacher's mass outside the list; rest: the factor of
+// 2^((x - st.m) c) there.  A student's row of nothing but mask values (lse below -1e30) has neither loss nor gradient.
+struct RowTerms { double left, total /* sum t + left */, all; float m, rest; bool outside, masked; };
+__device__ __forceinline__ RowTerms row_terms(const DistillArgs &a, double sum, const Stats &st, const Stats &sl, double g) {
     RowTerms r;
-    const bool outside = !(st.s == 0.f);
-    const double lse_r = outside ? (double)st.m * a.inv_t + log((double)st.s) : -INFINITY;
-    r.lse = log_add(l.lse, lse_r);
-    r.left = a.tail && outside ? fmax(1.0 - l.sum, 0.0) : 0.0;
-    r.masked = r.lse < -1e30;
-    double loss = 0.0;
-    for (int j = lane; j < a.k; j += 32)
-        if (l.t[j] != 0.0) loss += l.t[j] * (l.logt[j] - ((double)l.x[j] * a.inv_t - r.lse));
-    loss = warp_sum(loss);
-    const double p_r = outside ? exp(lse_r - r.lse) : 0.0;
-    if (r.left != 0.0) loss += r.left * (log(r.left) - (lse_r - r.lse));
-    r.loss = r.masked ? 0.0 : loss;
-    r.rest = outside && !r.masked ? (float)(g * ((l.sum + r.left) * p_r - r.left) / (double)st.s) : 0.f;
+    r.outside = !(st.s == 0.f);
+    const bool inside = !(sl.s == 0.f);
+    r.m = r.outside && inside ? fmaxf(st.m, sl.m) : r.outside ? st.m : sl.m;
+    const double from_rest = r.outside ? (double)st.s * (double)ex2(max_nan((st.m - r.m) * a.c, kFar)) : 0.0;
+    const double from_list = inside ? (double)sl.s * (double)ex2(max_nan((sl.m - r.m) * a.c, kFar)) : 0.0;
+    r.all = from_rest + from_list;
+    r.left = a.tail && r.outside ? fmax(1.0 - sum, 0.0) : 0.0;
+    r.total = sum + r.left;
+    r.masked = (!r.outside && !inside) || (double)r.m * a.inv_t < -1e30;
+    r.rest = r.outside && !r.masked ? (float)(g * (r.total * (from_rest / r.all) - r.left) / (double)st.s) : 0.f;
     return r;
 }
-// The gradient of listed entry j's token (the first of its entries writes it).
-__device__ __forceinline__ float listed_grad(const DistillArgs &a, const List &l, const RowTerms &r, double g, int j) {
+// The loss, by one warp; its three logarithms are one computation on three lanes.  ln of the student's mass outside the list is taken
+// from that mass's own sum, however small a part of the whole it is.
+template <int K>
+__device__ __forceinline__ double row_loss(const DistillArgs &a, const List<K> &l, const RowTerms &r, const Stats &st, int lane) {
+    const double o = log(lane == 0 ? r.all : lane == 1 ? (double)st.s : r.left);
+    const double log_all = __shfl_sync(0xffffffffu, o, 0), log_out = __shfl_sync(0xffffffffu, o, 1), log_left = __shfl_sync(0xffffffffu, o, 2);
+    double loss = 0.0;
+    for (int j = lane; j < a.k; j += 32)
+        if (l.t[j] != 0.0) loss += l.t[j] * (l.logt[j] - (((double)l.x[j] - (double)r.m) * a.inv_t - log_all));
+    loss = warp_sum(loss);
+    if (r.left != 0.0) loss += r.left * (log_left - (((double)st.m - (double)r.m) * a.inv_t + log_out - log_all));
+    return r.masked ? 0.0 : loss;
+}
+// The gradient of listed entry j's token, whose teacher's probability is that of all entries of it (`twice`: some token has several).
+template <int K>
+__device__ __forceinline__ float listed_grad(const DistillArgs &a, const List<K> &l, const RowTerms &r, double g, int j, bool twice) {
     if (r.masked) return 0.f;
-    double t = 0.0;
-    for (int i = j; i < a.k; ++i)
-        if (l.id[i] == l.id[j]) t += l.t[i];
-    const double p = l.x[j] == -INFINITY ? 0.0 : exp((double)l.x[j] * a.inv_t - r.lse);
-    return (float)(g * (p * (l.sum + r.left) - t));
+    double t = l.t[j];
+    if (twice) {
+        t = 0.0;
+        for (int i = 0; i < a.k; ++i)
+            if (l.id[i] == l.id[j]) t += l.t[i];
+    }
+    return (float)(g * ((double)ex2(max_nan((l.x[j] - r.m) * a.c, kFar)) / r.all * r.total - t));
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kDtThreads) distill_row_kernel(const DistillArgs a) {
-    constexpr int VE = Row<T>::VE, U = kDtUnroll;
-    extern __shared__ uint32_t s_bits[];              // a bit per position of this CTA's words: listed
-    __shared__ List s_list;
-    __shared__ Stats s_warp[kDtWarps];
-    __shared__ unsigned long long s_part[2];
-    __shared__ RowTerms s_terms;
-    pdl_enter();
+// A CTA's sums as they travel in its cluster.
+__device__ __forceinline__ unsigned long long pack_sums(const Stats &st) { return ((unsigned long long)__float_as_uint(st.s) << 32) | __float_as_uint(st.m); }
+__device__ __forceinline__ Stats unpack_sums(unsigned long long v) {
+    Stats st;
+    st.m = __uint_as_float((uint32_t)v);
+    st.s = __uint_as_float((uint32_t)(v >> 32));
+    st.w = 0.f;
+    return st;
+}
+
+// The CTAs of a cluster share a row; the second pass reads its words again, and says of them and of the gradient that they will not be
+// needed in L2, which leaves it to the words that wait for theirs.  (Tried instead and slower: words held in shared memory between the passes
+// by CTAs that walk over rows, 612 us for 4096 x 131072 bf16 against 456, the exponentials of the two passes no longer side by side.)
+template <typename T, int TH>
+__global__ void __launch_bounds__(TH, TH == 512 ? 2 : TH == 256 ? 5 : 10) distill_row_kernel(const DistillArgs a) {
+    constexpr int VE = Row<T>::VE, U = kDtUnroll, WARPS = TH / 32;
+    extern __shared__ uint32_t s_bits[];              // a bit per element of this CTA's words: listed
+    __shared__ List<kListMax> s_list;
+    __shared__ unsigned long long s_warp[WARPS], s_list_warp[WARPS], s_in[8], s_list_in[8];
     const uint32_t rank = rows_cluster_rank(), share = rows_cluster_size();
+    if (share > 1) rows_cluster_arrive();
+    pdl_enter();
     const long long row = blockIdx.x / share;
     const Row<T> r((const T *)a.x + row * a.x_row, a.V);
     T *dx = a.dx ? (T *)a.dx + row * a.dx_row : nullptr;
     const bool same = ((uintptr_t)(dx + r.head) & 15) == 0;
     const int begin = (int)((long long)r.words * rank / share), end = (int)((long long)r.words * (rank + 1) / share);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int id = (int)threadIdx.x < a.k ? a.index[row * a.k + threadIdx.x] : -1;
     const float weight = a.weight ? a.weight[row] : 1.f;
     const double g = (double)weight * a.inv_t / (double)a.B;
     const bool skip = weight == 0.f;                  // the same for the whole cluster
     const int edge = rank == 0 && threadIdx.x < Row<T>::EDGES ? r.edge(threadIdx.x) : -1;
     float at_edge = -INFINITY;
-
-    Stats st;
+    bool mine = false, twice = false;                 // this thread's entry is the one that stands for its token here; some token has several
+    Stats st, sl;
     st.reset();
+    sl.reset();
+    RowTerms terms = {};
+
     if (!skip) {
+        // The bits need the list's positions alone; what the teacher says of them is made ready by the first warp while the others read.
         const int bit_words = ((end - begin) * VE + 31) / 32;
-        for (int i = threadIdx.x; i < bit_words; i += kDtThreads) s_bits[i] = 0;
-        if (warp == 0) make_list<T>(a, row, s_list, lane, rank == 0);
+        for (int i = threadIdx.x; i < bit_words; i += TH) s_bits[i] = 0;
+        if ((int)threadIdx.x < a.k) s_list.id[threadIdx.x] = id >= 0 && id < a.V ? id : -1;
         __syncthreads();
-        if ((int)threadIdx.x < a.k && s_list.id[threadIdx.x] >= 0) {
-            const int at = s_list.id[threadIdx.x] - r.index(begin);
-            if (at >= 0 && at < (end - begin) * VE) atomicOr(&s_bits[at >> 5], 1u << (at & 31));
+        bool again = false;
+        if (id >= 0 && id < a.V) {
+            const int at = id - r.index(begin);
+            if (at >= 0 && at < (end - begin) * VE) {
+                const uint32_t bit = 1u << (at & 31);
+                again = atomicOr(&s_bits[at >> 5], bit) & bit;
+                mine = !again;
+            } else if (rank == 0 && (id < r.head || id >= r.index(r.words))) {
+                for (int i = 0; i < (int)threadIdx.x; ++i) again |= s_list.id[i] == id;      // on the edges: few, so by looking
+                mine = !again;
+            }
         }
         if (edge >= 0) {
             at_edge = to_f32(r.at(edge));
             bool out = false;
             for (int j = 0; j < a.k; ++j) out |= s_list.id[j] == edge;
             const float x[2] = {out ? -INFINITY : at_edge, -INFINITY};
-            if (x[0] > st.m) st.raise(x[0], a.c);
+            if (x[0] > st.m) st.m = x[0];
             accumulate<2, false>(st, x, a.c);
         }
-        __syncthreads();
+        twice = __syncthreads_or(again);
+        if (mine) {
+            const float x[2] = {to_f32(r.at(id)), -INFINITY};
+            if (x[0] > sl.m) sl.m = x[0];
+            accumulate<2, false>(sl, x, a.c);
+        }
         const uint8_t *bytes = reinterpret_cast<const uint8_t *>(s_bits);
         auto word = [&](const uint4 &v, int i0) {
             float f[VE];
@@ -187,65 +221,55 @@ __global__ void __launch_bounds__(kDtThreads) distill_row_kernel(const DistillAr
             accumulate<VE, false>(st, f, a.c);
         };
         int w = begin + (int)threadIdx.x;
-        for (; w + (U - 1) * kDtThreads < end; w += kDtThreads * U) {
+        for (; w + (U - 1) * TH < end; w += TH * U) {
             uint4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = r.load(w + u * kDtThreads);
+            for (int u = 0; u < U; ++u) v[u] = r.load(w + u * TH);
 #pragma unroll
-            for (int u = 0; u < U; ++u) word(v[u], w + u * kDtThreads - begin);
+            for (int u = 0; u < U; ++u) word(v[u], w + u * TH - begin);
         }
-        for (; w < end; w += kDtThreads) word(r.load(w), w - begin);
+        for (; w < end; w += TH) word(r.load(w), w - begin);
+        if (warp == 0) make_list<T>(a, row, s_list, lane, rank == 0);
         warp_join(st, a.c);
-        if (lane == 0) s_warp[warp] = st;
+        warp_join(sl, a.c);
+        if (lane == 0) { s_warp[warp] = pack_sums(st); s_list_warp[warp] = pack_sums(sl); }
         __syncthreads();
-        if (warp == 0) {
+        // each warp joins the warps' sums for itself, which saves a barrier
+        st.reset();
+        sl.reset();
+        if (lane < WARPS) { st = unpack_sums(s_warp[lane]); sl = unpack_sums(s_list_warp[lane]); }
+        warp_join(st, a.c);
+        warp_join(sl, a.c);
+        if (share > 1) {
+            // every CTA hands its sums to all
+            rows_cluster_wait();                      // they have started
+            if (warp == 0 && lane < (int)share) {
+                st_peer_u64(&s_in[rank], lane, pack_sums(st));
+                st_peer_u64(&s_list_in[rank], lane, pack_sums(sl));
+            }
+            // every CTA of the cluster has read what it gathers before any writes a gradient, which may lie where the logits do
+            rows_cluster_sync();
             st.reset();
-            if (lane < kDtWarps) st = s_warp[lane];
+            sl.reset();
+            if (lane < (int)share) { st = unpack_sums(s_in[lane]); sl = unpack_sums(s_list_in[lane]); }
             warp_join(st, a.c);
-            if (lane == 0) {
-                s_warp[0] = st;
-                s_part[0] = ((unsigned long long)__float_as_uint(st.s) << 32) | __float_as_uint(st.m);
-            }
+            warp_join(sl, a.c);
         }
-    }
-    // every CTA of the cluster has read what it gathers before any writes a gradient, which may lie where the logits do
-    if (share > 1) {
-        __syncthreads();
-        rows_cluster_sync();
-        if (!skip && warp == 0) {
-            st.reset();
-            for (uint32_t o = 0; o < share; ++o) {                // in the same order everywhere
-                const unsigned long long p0 = ld_peer_u64(&s_part[0], o);
-                Stats b;
-                b.m = __uint_as_float((uint32_t)p0);
-                b.s = __uint_as_float((uint32_t)(p0 >> 32));
-                b.w = 0.f;
-                st.join(b, a.c);
-            }
-            if (lane == 0) s_warp[0] = st;
-        }
-        __syncthreads();
-        rows_cluster_sync();
-    } else
-        __syncthreads();
-    if (skip) {
-        if (threadIdx.x == 0 && rank == 0) a.row_loss[row] = 0.f;
-        if (!dx) return;
+        terms = row_terms(a, s_list.sum, st, sl, g);
     } else {
-        if (warp == 0) {
-            const RowTerms t = row_terms(a, s_list, s_warp[0], g, lane);
-            if (lane == 0) {
-                s_terms = t;
-                if (rank == 0) a.row_loss[row] = (float)t.loss;
-            }
+        if (share > 1) {
+            rows_cluster_wait();
+            rows_cluster_sync();
         }
-        if (!dx) return;
-        __syncthreads();
     }
-    const float rest = skip ? 0.f : s_terms.rest, m = skip ? 0.f : s_warp[0].m;
-    auto grad = [&](float x) { return rest * ex2(max_nan((x - m) * a.c, kFar)); };
+    if (rank == 0 && warp == WARPS - 1) {
+        const double loss = skip ? 0.0 : row_loss(a, s_list, terms, st, lane);
+        if (lane == 0) a.row_loss[row] = (float)loss;
+    }
+    if (!dx) return;
+    auto grad = [&](float x) { return terms.rest * ex2(max_nan((x - st.m) * a.c, kFar)); };
     auto put = [&](int w, const float *f) {
-        if (same) *reinterpret_cast<uint4 *>(dx + r.index(w)) = pack_vec<T>(f);
+        if (same) __stcs(reinterpret_cast<uint4 *>(dx + r.index(w)), pack_vec<T>(f));
         else {
 #pragma unroll
             for (int i = 0; i < VE; ++i) dx[r.index(w) + i] = from_f32<T>(f[i]);
@@ -260,75 +284,105 @@ __global__ void __launch_bounds__(kDtThreads) distill_row_kernel(const DistillAr
             for (int i = 0; i < VE; ++i) f[i] = grad(f[i]);
             put(at, f);
         };
-        for (; w + (U - 1) * kDtThreads < end; w += kDtThreads * U) {
+        for (; w + (U - 1) * TH < end; w += TH * U) {
             uint4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = r.load(w + u * kDtThreads);
+            for (int u = 0; u < U; ++u) v[u] = r.load_last(w + u * TH);
 #pragma unroll
-            for (int u = 0; u < U; ++u) word(v[u], w + u * kDtThreads);
+            for (int u = 0; u < U; ++u) word(v[u], w + u * TH);
         }
-        for (; w < end; w += kDtThreads) word(r.load(w), w);
+        for (; w < end; w += TH) word(r.load(w), w);
     } else {
         const float zeros[VE] = {};
-        for (; w < end; w += kDtThreads) put(w, zeros);
+        for (; w < end; w += TH) put(w, zeros);
     }
     if (edge >= 0) dx[edge] = from_f32<T>(skip ? 0.f : grad(at_edge));
     if (skip) return;
     __syncthreads();
-    if ((int)threadIdx.x < a.k && s_list.first[threadIdx.x]) {
-        const int id = s_list.id[threadIdx.x], at = id - r.index(begin);
-        const bool here = (at >= 0 && at < (end - begin) * VE) || (rank == 0 && (id < r.head || id >= r.index(r.words)));
-        if (here)
-            dx[id] = from_f32<T>(listed_grad(a, s_list, s_terms, g, threadIdx.x));
-    }
+    if (mine) dx[s_list.id[threadIdx.x]] = from_f32<T>(listed_grad(a, s_list, terms, g, threadIdx.x, twice));
 }
 
-// A warp per row of at most 32 * E values; lane l holds those at l, l + 32, ..., bit i of `out` says that the i-th is listed.
-template <typename T, int E>
-__global__ void __launch_bounds__(128) distill_warp_kernel(const DistillArgs a) {
-    __shared__ List s_list[4];
-    pdl_enter();
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (row >= a.rows) return;
+// A warp per row of at most 32 * E values; lane l holds those at l, l + 32, ..., bit i of `out` says that the i-th is listed.  Returns the
+// row's loss times its weight, in lane 0.
+template <typename T, int E, int K>
+__device__ __forceinline__ double distill_row_of_warp(const DistillArgs &a, long long row, List<K> &l, int lane) {
     const T *x = (const T *)a.x + row * a.x_row;
     T *dx = a.dx ? (T *)a.dx + row * a.dx_row : nullptr;
     const float weight = a.weight ? a.weight[row] : 1.f;
     if (weight == 0.f) {
         if (lane == 0) a.row_loss[row] = 0.f;
         for (int i = lane; dx && i < a.V; i += 32) dx[i] = from_f32<T>(0.f);
-        return;
+        return 0.0;
     }
     const double g = (double)weight * a.inv_t / (double)a.B;
-    List &l = s_list[threadIdx.x >> 5];
     float f[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) f[i] = lane + 32 * i < a.V ? to_f32(x[lane + 32 * i]) : -INFINITY;
     make_list<T>(a, row, l, lane, true);
     uint32_t out = 0;
+    bool again = false;
     for (int j = 0; j < a.k; ++j) {
         const int id = l.id[j];
-        if (id >= 0 && (id & 31) == lane) out |= 1u << (id >> 5);
+        if (id >= 0 && (id & 31) == lane) {
+            again |= (out >> (id >> 5)) & 1u;
+            out |= 1u << (id >> 5);
+        }
     }
-    Stats st;
+    const bool twice = __any_sync(0xffffffffu, again);
+    Stats st, sl;
     st.reset();
-    float m = kLowest;
+    sl.reset();
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        if ((out >> i) & 1u) f[i] = -INFINITY;
-        m = fmaxf(m, f[i]);
+        if ((out >> i) & 1u) sl.m = fmaxf(sl.m, f[i]);
+        else st.m = fmaxf(st.m, f[i]);
     }
-    st.raise(m, a.c);
-    accumulate<E, false>(st, f, a.c);
-    warp_join(st, a.c);
-    const RowTerms t = row_terms(a, l, st, g, lane);
-    if (lane == 0) a.row_loss[row] = (float)t.loss;
-    if (!dx) return;
+    float in[E];
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-        if (lane + 32 * i < a.V && !((out >> i) & 1u)) dx[lane + 32 * i] = from_f32<T>(t.rest * ex2(max_nan((f[i] - st.m) * a.c, kFar)));
-    for (int j = lane; j < a.k; j += 32)
-        if (l.first[j]) dx[l.id[j]] = from_f32<T>(listed_grad(a, l, t, g, j));
+    for (int i = 0; i < E; ++i) {
+        in[i] = (out >> i) & 1u ? f[i] : -INFINITY;
+        if ((out >> i) & 1u) f[i] = -INFINITY;
+    }
+    accumulate<E, false>(st, f, a.c);
+    accumulate<E, false>(sl, in, a.c);
+    warp_join(st, a.c);
+    warp_join(sl, a.c);
+    const RowTerms t = row_terms(a, l.sum, st, sl, g);
+    const double loss = row_loss(a, l, t, st, lane);
+    if (lane == 0) a.row_loss[row] = (float)loss;
+    if (dx) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (lane + 32 * i < a.V && !((out >> i) & 1u)) dx[lane + 32 * i] = from_f32<T>(t.rest * ex2(max_nan((f[i] - st.m) * a.c, kFar)));
+        // (entries of one token write the same value)
+        for (int j = lane; j < a.k; j += 32)
+            if (l.id[j] >= 0) dx[l.id[j]] = from_f32<T>(listed_grad(a, l, t, g, j, twice));
+    }
+    return (double)weight * (double)(float)loss;
+}
+// Four rows a CTA.
+template <typename T, int E, int K>
+__global__ void __launch_bounds__(128) distill_warp_kernel(const DistillArgs a) {
+    __shared__ List<K> s_list[4];
+    pdl_enter();
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row < a.rows) distill_row_of_warp<T, E, K>(a, row, s_list[threadIdx.x >> 5], threadIdx.x & 31);
+}
+// A node's rows, at most 32, and its loss, with no launch more.
+template <typename T, int E, int K>
+__global__ void __launch_bounds__(1024) distill_node_kernel(const DistillArgs a, float *__restrict__ loss) {
+    extern __shared__ __align__(16) unsigned char s_lists[];
+    __shared__ double s_loss[32];
+    pdl_enter();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const double l = distill_row_of_warp<T, E, K>(a, (long long)blockIdx.x * a.B + warp, reinterpret_cast<List<K> *>(s_lists)[warp], lane);
+    if (lane == 0) s_loss[warp] = l;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = 0.0;
+        for (int b = 0; b < a.B; ++b) s += s_loss[b];
+        loss[blockIdx.x] = (float)(s / (double)a.B);
+    }
 }
 
 // loss[n] = sum_b weight * row_loss / B, rows of weight 0 left out; sums in double, in a fixed order.
@@ -374,27 +428,46 @@ extern "C" lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, co
     a.inv_t = 1.0 / (double)temperature; a.c = (float)(1.4426950408889634 / (double)temperature);
     a.value = teacher_logprob; a.index = teacher_index; a.weight = row_weight; a.row_loss = row_loss; a.dev_status = dev_status;
     const cudaStream_t st = as_stream(stream);
+    bool done = false;
     const lpdt_status s = with_dtype(dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
         if (V <= 1024) {
+            // one launch for a node's rows and its loss where a CTA has a warp for each and they are short
+            if (B <= 32 && V <= 256 && k <= 32) {
+                auto fn = V <= 64 ? distill_node_kernel<T, 2, 32> : distill_node_kernel<T, 8, 32>;
+                launch_k(fn, (unsigned)nodes, 32 * B, B * sizeof(List<32>), st, a, loss);
+                LPDT_LAUNCH_CHECK();
+                done = true;
+                return LPDT_OK;
+            }
             const unsigned grid = (unsigned)ceil_div(rows, 4);
-            if (V <= 64) launch_k(distill_warp_kernel<T, 2>, grid, 128, 0, st, a);
-            else if (V <= 256) launch_k(distill_warp_kernel<T, 8>, grid, 128, 0, st, a);
-            else launch_k(distill_warp_kernel<T, 32>, grid, 128, 0, st, a);
+            if (V <= 64) launch_k(distill_warp_kernel<T, 2, kListMax>, grid, 128, 0, st, a);
+            else if (V <= 256) launch_k(distill_warp_kernel<T, 8, kListMax>, grid, 128, 0, st, a);
+            else launch_k(distill_warp_kernel<T, 32, kListMax>, grid, 128, 0, st, a);
         } else {
             const int cs = row_share(rows, (int64_t)V * sizeof(T), 4, 4096);
-            const size_t smem = align_up(ceil_div((int64_t)V + 2 * Row<T>::VE, cs) / 8 + 16, 16);
-            static PerDeviceOnce attr;
-            int dev;
-            if (attr.pending(&dev)) {
-                LPDT_CUDA(cudaFuncSetAttribute(distill_row_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDtSmem));
-                attr.mark(dev);
-            }
-            launch_k_cluster(distill_row_kernel<T>, (unsigned)(rows * cs), kDtThreads, smem, st, cs, a);
+            const size_t smem = align_up(ceil_div((int64_t)V, cs) / 8 + 16, 16);
+            // threads by what a CTA reads: few for short rows, whose barriers and joins cost more than the reading
+            const int64_t bytes = (int64_t)V * (int64_t)sizeof(T) / cs;
+            auto go = [&](auto threads) -> lpdt_status {
+                constexpr int TH = decltype(threads)::value;
+                static PerDeviceOnce attr;
+                int dev;
+                if (attr.pending(&dev)) {
+                    LPDT_CUDA(cudaFuncSetAttribute(distill_row_kernel<T, TH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDtSmem));
+                    attr.mark(dev);
+                }
+                launch_k_cluster(distill_row_kernel<T, TH>, (unsigned)(rows * cs), TH, smem, st, cs, a);
+                return LPDT_OK;
+            };
+            const lpdt_status s = bytes <= 16384 ? go(std::integral_constant<int, 128>()) : bytes <= 65536 ? go(std::integral_constant<int, 256>())
+                                                                                          : go(std::integral_constant<int, 512>());
+            if (s != LPDT_OK) return s;
         }
         LPDT_LAUNCH_CHECK();
         return LPDT_OK;
     });
+    if (done) return LPDT_OK;
     if (s != LPDT_OK) return s;
     launch_k(distill_loss_kernel, (unsigned)nodes, 256, 0, st, (int)B, (const float *)row_loss, row_weight, loss);
     LPDT_LAUNCH_CHECK();

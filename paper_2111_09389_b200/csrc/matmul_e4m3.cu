@@ -12,7 +12,7 @@
 // are written and read in 112 cycles).  G = 1: one SM, for what is too small to fill pairs; a cluster of SPLIT CTAs may share a tile's K
 // and add their accumulators through distributed shared memory, in the order of the CTAs.
 //
-// Two accumulators of up to 240 columns (the epilogue of one tile runs under the products of the next) and two sets of scale factors
+// Two accumulators of up to 224 columns (the epilogue of one tile runs under the products of the next) and four sets of scale factors
 // fill the 512 columns of tensor memory.
 //
 // Roles per CTA: warp 0 fetches codes (TMA), warp 1 copies scale factors to tensor memory and issues the products, warp 2 brings the
@@ -23,7 +23,7 @@
 namespace lpdt {
 namespace tc {
 
-constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleBytes = 1536, kMmScaleSlots = 4, kMmMaxRows = 240 /*2 * 240 + 32 <= 512*/, kMmRaster = 8;
+constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleBytes = 1536, kMmScaleSlots = 4, kMmMaxRows = 224 /*2 * 224 + 4 * 16 <= 512*/, kMmRaster = 8;
 constexpr size_t kMmSmem = 227 * 1024;
 
 struct MmParams {
@@ -209,33 +209,42 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             const uint32_t idesc = idesc_mx_e4m3(128 * G, p.bn);
             const uint64_t tpl = smem_desc(0, 16, 1024, 2), sc_tpl = smem_desc(0, 16, 128, 0);
             const uint32_t sf0 = tmem_base + 2 * p.bn;
-            int st = 0; uint32_t ph = 0, tcount = 0, group = 0;
-            for (int tile = first; tile < total && !ctl->abort_flag; tile += step, ++tcount) {
+            // Groups of four blocks of K, counted over all tiles: `copied` have their factors in tensor memory or on their way.  A group's are
+            // copied one group ahead of its products, which then do not wait for the copy.
+            const uint32_t per_tile = (uint32_t)(((k_end - 1) >> 2) - (k_begin >> 2) + 1);
+            const uint32_t groups = first < total ? per_tile * (uint32_t)((total - 1 - first) / step + 1) : 0u;
+            uint32_t group = 0, copied = 0;
+            auto copy = [&]() {
+                const uint32_t slot = copied & (kMmScaleSlots - 1), turn = copied / kMmScaleSlots;
+                // the columns' and the slot's last group, kMmScaleSlots before this one, has been used
+                if (turn && !mbar_wait(smem_u32(&ctl->sf_done[slot]), (turn - 1) & 1, &ctl->abort_flag, p.dev_status)) return false;
+                if (!mbar_wait(smem_u32(&ctl->sf_full[slot]), turn & 1, &ctl->abort_flag, p.dev_status)) return false;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t sc = smem_u32(scales + (size_t)slot * kMmScaleBytes) >> 4, sf = sf0 + slot * 16;
+                    mm_copy_scales<G>(sf, sc_tpl | (sc & 0x3FFFu));
+                    mm_copy_scales<G>(sf + 4, sc_tpl | ((sc + 32) & 0x3FFFu));
+                    if (p.bn > 128) mm_copy_scales<G>(sf + 8, sc_tpl | ((sc + 64) & 0x3FFFu));
+                }
+                __syncwarp();
+                ++copied;
+                return true;
+            };
+            int st = 0; uint32_t ph = 0, tcount = 0;
+            bool ok = true;
+            for (int tile = first; tile < total && ok && !ctl->abort_flag; tile += step, ++tcount) {
                 const int acc = tcount & 1;
                 if (!mbar_wait(smem_u32(&ctl->tmem_empty[acc]), ((tcount >> 1) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) break;
                 tc_fence_after();
-                bool ok = true;
-                for (int kb = k_begin; kb < k_end; ++kb) {
-                    if (kb == k_begin || (kb & 3) == 0) {
-                        // The next four blocks' factors, into the set of columns that the group before last has left: its products are
-                        // done (those of the last group keep the tensor cores busy meanwhile).
-                        const int slot = group & (kMmScaleSlots - 1), old = (group - 2) & (kMmScaleSlots - 1);
-                        if (group >= 2 && !mbar_wait(smem_u32(&ctl->sf_done[old]), ((group - 2) / kMmScaleSlots) & 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
-                        if (!mbar_wait(smem_u32(&ctl->sf_full[slot]), (group / kMmScaleSlots) & 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint32_t sc = smem_u32(scales + (size_t)slot * kMmScaleBytes) >> 4, sf = sf0 + (group & 1) * 16;
-                            mm_copy_scales<G>(sf, sc_tpl | (sc & 0x3FFFu));
-                            mm_copy_scales<G>(sf + 4, sc_tpl | ((sc + 32) & 0x3FFFu));
-                            if (p.bn > 128) mm_copy_scales<G>(sf + 8, sc_tpl | ((sc + 64) & 0x3FFFu));
-                        }
-                        __syncwarp();
-                        ++group;
-                    }
-                    if (!mbar_wait(smem_u32(&ctl->full[st]), ph, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
+                for (int kb = k_begin; kb < k_end && ok; ++kb) {
+                    const bool fresh = kb == k_begin || (kb & 3) == 0;
+                    if (fresh && copied == group) ok = copy();
+                    if (!ok || !mbar_wait(smem_u32(&ctl->full[st]), ph, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
                     tc_fence_after();
+                    const uint32_t slot = group & (kMmScaleSlots - 1);
+                    const bool last = (kb & 3) == 3 || kb == k_end - 1;
                     if (elect_one()) {
-                        const uint32_t id = idesc | ((uint32_t)(kb & 3) << 4) | ((uint32_t)(kb & 3) << 29), sf = sf0 + ((group - 1) & 1) * 16;
+                        const uint32_t id = idesc | ((uint32_t)(kb & 3) << 4) | ((uint32_t)(kb & 3) << 29), sf = sf0 + slot * 16;
                         uint32_t l = smem_u32(data + (size_t)st * p.slot) >> 4, r = l + (kMmLaneBytes >> 4);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
@@ -243,13 +252,14 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
                             l += 2; r += 2;
                         }
                         mm_commit<G>(smem_u32(&ctl->empty[st]));
-                        if ((kb & 3) == 3 || kb == k_end - 1) mm_commit<G>(smem_u32(&ctl->sf_done[(group - 1) & (kMmScaleSlots - 1)]));
+                        if (last) mm_commit<G>(smem_u32(&ctl->sf_done[slot]));
                         if (kb == k_end - 1) mm_commit<G>(smem_u32(&ctl->tmem_full[acc]));
                     }
                     __syncwarp();
                     if (++st == p.stages) { st = 0; ph ^= 1; }
+                    if (fresh && copied == group + 1 && copied < groups) ok = copy();
+                    if (last) ++group;
                 }
-                if (!ok) break;
             }
         }
     } else if (warp == 2) {
@@ -461,7 +471,7 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     p.slot = kMmLaneBytes + (int)align_up((size_t)(plan.bn / plan.g) * 128, 1024);
     p.stages = (int)((kMmSmem - 1024 - kMmScaleSlots * kMmScaleBytes) / p.slot);
     if (p.stages > kMmMaxStages) p.stages = kMmMaxStages;
-    for (p.tmem_cols = 64; p.tmem_cols < 2 * plan.bn + 32; p.tmem_cols *= 2) {}
+    for (p.tmem_cols = 128; p.tmem_cols < 2 * plan.bn + kMmScaleSlots * 16; p.tmem_cols *= 2) {}
     p.sA = sA; p.sB = sB; p.spitch = (int)lpdt_e4m3_scale_pitch(K);
     p.bias = bias; p.bias_node = nodes == 1 ? 0 : bias_node_stride;
     p.addend = addend; p.C = C; p.c_node = nodes == 1 ? 0 : c_node_stride; p.c_row = M == 1 ? 0 : c_row_stride;

@@ -47,6 +47,7 @@ struct Row {
         words = (V - head) / VE;
     }
     __device__ __forceinline__ uint4 load(int w) const { return reinterpret_cast<const uint4 *>(base)[w]; }
+    __device__ __forceinline__ uint4 load_last(int w) const { return __ldcs(reinterpret_cast<const uint4 *>(base) + w); }    // not to be read again
     __device__ __forceinline__ int index(int w) const { return w * VE + head; }          // of the word's first element
     // Index of the i-th element of the edges (i < EDGES), -1 where there is none.
     __device__ __forceinline__ int edge(int i) const {

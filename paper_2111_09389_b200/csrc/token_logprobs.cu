@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogprobBwdArgs 
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (w0 + u * 32 < r.words) v[u] = r.load(w0 + u * 32);
+        if (w0 + u * 32 < r.words) v[u] = r.load_last(w0 + u * 32);
     const int t = a.tokens ? a.tokens[row] : -1;
     const bool some = t >= 0 && t < a.V;
     const float lse = a.lse[row], g = a.g_logprob && some ? a.g_logprob[row] : 0.f;
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogprobBwdArgs 
         const int first = r.index(w);
 #pragma unroll
         for (int i = 0; i < VE; ++i) f[i] = grad(f[i], first + i);
-        if (same) *reinterpret_cast<uint4 *>(dx + first) = pack_vec<T>(f);
+        if (same) __stcs(reinterpret_cast<uint4 *>(dx + first), pack_vec<T>(f));
         else {
 #pragma unroll
             for (int i = 0; i < VE; ++i) dx[first + i] = from_f32<T>(f[i]);

@@ -282,10 +282,11 @@ def test_distill(nodes, B, V, k, temperature, tail, dtype):
 
 @pytest.mark.parametrize("tail", [True, False])
 @pytest.mark.parametrize("V", [12, 200, 1000, 4099, 90001])
-def test_distill_of_hard_lists(V, tail):
+@pytest.mark.parametrize("B", [9, 170])                       # few rows are shared by clusters
+def test_distill_of_hard_lists(V, tail, B):
     """Tokens listed twice, short and empty lists, ids out of range, rows of weight 0, a teacher sure of itself, a student that has
     (nearly) all of its mass on the list, masked tokens on and off the list, a student's row of nothing but masks."""
-    nodes, B, k = 2, 9, 8
+    nodes, k = 2, 8
     x = logits_of(nodes * B, V, torch.float32, V).view(nodes, B, V)
     value, index = lists_of(nodes, B, V, k, V + 1)
     weight = np.ones((nodes, B), np.float32)
@@ -307,7 +308,38 @@ def test_distill_of_hard_lists(V, tail):
     value[1, 3] = -float("inf")
     value[1, 4, 2] = -float("inf")
     x[1, 5, V // 2] = -float("inf")
+    if B > 100:
+        for a in (x, value, index, weight):
+            a[0, 140:149], a[1, 150:159] = a[0, :9], a[1, :9]
+        weight[:, 9::13] = 0
     check_distill(x, value, index, tail, weight)
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.bfloat16, 16400), (torch.bfloat16, 131072), (torch.float16, 50021), (torch.float32, 9003), (torch.float32, 70001),
+                                     (torch.float32, 131200)])
+def test_distill_of_many_long_rows(dtype, V):
+    """Hundreds of rows at every number of threads, odd strides, in place; weights that are 0 or negative."""
+    nodes, B, k, stride = 3, 113, 20, V + 1 + V % 2
+    flat = torch.full((2 + nodes * B * stride,), 7.0, dtype=dtype, device="cuda")
+    view = torch.as_strided(flat, (nodes, B, V), (B * stride, stride, 1), 2)
+    x = logits_of(nodes * B, V, dtype, V).view(nodes, B, V)
+    view.copy_(x)
+    value, _ = lists_of(nodes, B, 1000, k, V)
+    index = np.random.default_rng(V).integers(0, V, (nodes, B, k)).astype(np.int32)
+    weight = np.random.default_rng(1).uniform(0.5, 2, (nodes, B)).astype(np.float32)
+    weight[:, ::4], weight[:, 1::8] = 0, -1
+    loss, row_loss = torch.empty(nodes, device="cuda"), torch.empty(nodes, B, device="cuda")
+    api.lpdt_distill_topk(nodes, B, V, view, k, torch.from_numpy(value).cuda(), torch.from_numpy(index).cuda(), loss, row_loss, dlogits=view,
+                          row_weight=torch.from_numpy(weight).cuda(), row_stride=stride, dlogits_row_stride=stride)
+    result = view.clone()
+    view.fill_(7)
+    assert (flat == 7).all()
+    some = slice(0, None, 16)
+    L, R, G = heads.distill_topk(x[:, some].double().numpy(), value[:, some], index[:, some], True, 1.0, weight[:, some])
+    G = G * G.shape[1] / B
+    within(row_loss[:, some], R, 6 * SUM(V) + 2 * U * np.abs(R))
+    within(loss, (row_loss.double().cpu().numpy() * weight).mean(1), 2 * U * np.abs(row_loss.cpu().numpy() * weight).mean(1) + 1e-30)
+    within(result[:, some], G, 8 * SUM(V) / B + torch.finfo(dtype).eps / 2 * np.abs(G) + 2.0 ** -25 * (dtype == torch.float16))
 
 
 @pytest.mark.parametrize("V", [10, 700, 3000, 50000])
