@@ -52,42 +52,47 @@ constexpr int kLpUnroll = 4, kTopMax = 128;
 // What could be among the k best of a row, and then the k best in order.
 template <int TH> struct TopList {
     static constexpr int CAP = TH < 256 ? 8 * TH : 2048;
-    __align__(16) unsigned long long key[CAP];
-    int count;
+    __align__(16) unsigned long long key[CAP + 8];
+    unsigned long long best[kTopMax];
+    static constexpr int ITEMS = 4 * TH;
+    int item[ITEMS];                             // words to look through: twice the first, 1 more for a word by itself and not a turn
+    int again[TH];                               // threads whose every word has to be
+    int count, items, agains;
 };
-// Cuts the list of n keys to its k best, in order.  Each thread ranks its share by counting the larger ones: n is near k.
+// (The code behind a row's end runs once a row: a row by itself waits for each of its instructions to be fetched, so it is written to be
+// short, in loops that are not unrolled.  Unrolled over a thread's words and keys the top 20 of one row took 10 us more than none, this 5.)
+
+// The number of the n keys of the list that are larger; n is padded with zeros to a multiple of 8.
+template <int TH>
+__device__ __forceinline__ int larger_keys(const TopList<TH> &l, int n, unsigned long long mine) {
+    const ulonglong2 *keys = reinterpret_cast<const ulonglong2 *>(l.key);
+    int r = 0;
+#pragma unroll 1
+    for (int j = 0; j < n / 2; j += 4) {
+        ulonglong2 k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = keys[j + i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r += (k[i].x > mine) + (k[i].y > mine);
+    }
+    return r;
+}
+// Cuts the list of n keys to its k best, in order, by counting the larger ones of each: n is near k.
 template <int TH>
 __device__ __noinline__ void top_cut(TopList<TH> &l, int n, int k) {
-    constexpr int PER = TopList<TH>::CAP / TH;
-    if (n <= TH) {
-        const unsigned long long mine = (int)threadIdx.x < n ? l.key[threadIdx.x] : 0;
-        int r = TH;
-        if ((int)threadIdx.x < n) {
-            r = 0;
-#pragma unroll 4
-            for (int j = 0; j < n; ++j) r += l.key[j] > mine;
-        }
-        __syncthreads();
-        if (r < k) l.key[r] = mine;
-    } else {
-        unsigned long long mine[PER];
-        int rank[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int at = threadIdx.x + i * TH;
-            rank[i] = TopList<TH>::CAP;
-            if (at >= n) continue;
-            mine[i] = l.key[at];
-            int r = 0;
-            for (int j = 0; j < n; ++j) r += l.key[j] > mine[i];
-            rank[i] = r;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (rank[i] < k) l.key[rank[i]] = mine[i];
+    const int padded = (n + 7) & ~7;
+    if ((int)threadIdx.x < padded - n) l.key[n + threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int at = threadIdx.x; at < n; at += TH) {
+        const unsigned long long mine = l.key[at];
+        const int r = larger_keys(l, padded, mine);
+        if (r < k) l.best[r] = mine;
     }
-    if (threadIdx.x == 0) l.count = n < k ? n : k;
+    __syncthreads();
+    n = n < k ? n : k;
+    if ((int)threadIdx.x < n) l.key[threadIdx.x] = l.best[threadIdx.x];
+    if (threadIdx.x == 0) l.count = n;
     __syncthreads();
 }
 
@@ -105,115 +110,75 @@ struct Best {
         w1 = first ? at : w1;
     }
 };
-// The best key of a word whose first element has this index (0: nothing but NaN); calls, so that the kernel around them keeps its registers.
-template <typename T>
-__device__ __noinline__ unsigned long long word_best(uint4 v, int index) {
-    constexpr int VE = Row<T>::VE;
-    float x[VE];
-    unpack_vec<T>(v, x);
-    unsigned long long best = 0;
-#pragma unroll
-    for (int i = 0; i < VE; ++i)
-        if (x[i] == x[i]) {
-            const unsigned long long key = top_key(x[i], index + i);
-            if (key > best) best = key;
-        }
-    return best;
-}
-template <typename T, int TH>
-__device__ __noinline__ void word_offer(uint4 v, int index, unsigned long long floor_key, float floor_v, TopList<TH> &l) {
-    constexpr int VE = Row<T>::VE;
-    float x[VE];
-    unpack_vec<T>(v, x);
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-        if (!(x[i] >= floor_v)) continue;
-        const unsigned long long key = top_key(x[i], index + i);
-        if (key < floor_key) continue;
-        const int to = atomicAdd(&l.count, 1);
-        if (to < TopList<TH>::CAP) l.key[to] = key;
-    }
-}
-// A thread takes its words in turns of kLpUnroll, TH apart, and the last few one by one.  The words of the turn from w on; those of no turn
-// are NaN.
-template <typename T, int TH>
-__device__ __forceinline__ void load_turn(const Row<T> &r, int w, int end, uint4 (&v)[kLpUnroll]) {
-    const bool full = w + (kLpUnroll - 1) * TH < end;
-    v[0] = r.load(w);
-#pragma unroll
-    for (int u = 1; u < kLpUnroll; ++u) v[u] = full ? r.load(w + u * TH) : same_word(from_f32<T>(NAN));
-}
-template <typename T, int TH>
-__device__ __forceinline__ void offer(const Row<T> &r, int w, int end, unsigned long long floor_key, float floor_v, TopList<TH> &l) {
-    uint4 v[kLpUnroll];
-    load_turn<T, TH>(r, w, end, v);
-    uint32_t in = 0;
-#pragma unroll
-    for (int u = 0; u < kLpUnroll; ++u) in |= (uint32_t)(vec_max<T>(v[u]) >= floor_v) << u;
-    for (; in; in &= in - 1) {                   // one word, as a rule: one call for the warp's lanes
-        const int u = __ffs(in) - 1;
-        const uint4 x = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
-        word_offer<T, TH>(x, r.index(w + u * TH), floor_key, floor_v, l);
-    }
-}
-// Puts everything that reaches the floor on the list (`edges`: the row's edges too); its new length (which may exceed the room).  What reaches the floor lies in the turns
-// that reach it.  A thread whose second turn does may have more: all of its turns are read again, by everyone.
+// Puts everything that reaches the floor on the list (`edges`: the row's edges too); its new length, which may exceed the room.  What reaches
+// the floor lies in the turns that reach it; a thread whose second best turn does may have more, so all of its words are looked at.
+// A warp looks through an item, an element a lane.
 template <typename T, int TH>
 __device__ __noinline__ int collect(const Row<T> r, int begin, int end, bool edges, const Best b, unsigned long long floor_key, TopList<TH> &l) {
-    __shared__ int s_again[TH], s_agains;
+    constexpr int VE = Row<T>::VE;
     const float floor_v = floor_key ? key_value(floor_key) : -INFINITY;
     const uint32_t floor_i = (uint32_t)key_index(floor_key);          // the last position that counts among equal ones
-    const int tid = threadIdx.x;
-    if (tid == 0) { l.count = 0; s_agains = 0; }
+    const int tid = threadIdx.x, lane = tid & 31;
+    if (tid == 0) l.count = l.items = l.agains = 0;
     __syncthreads();
     auto in = [&](float v, int w) { return v > floor_v || (v == floor_v && (uint32_t)r.index(w) <= floor_i); };
-    if (in(b.v2, b.w2)) s_again[atomicAdd(&s_agains, 1)] = begin + tid;
-    else if (in(b.v1, b.w1)) offer(r, b.w1, end, floor_key, floor_v, l);
-    if (edges && tid < Row<T>::EDGES && r.edge(tid) >= 0) {
-        const float x = to_f32(r.at(r.edge(tid)));
-        const unsigned long long key = top_key(x, r.edge(tid));
-        if (x >= floor_v && key >= floor_key) {
-            const int to = atomicAdd(&l.count, 1);
-            if (to < TopList<TH>::CAP) l.key[to] = key;
-        }
+    if (in(b.v1, b.w1)) {
+        if (in(b.v2, b.w2)) l.again[atomicAdd(&l.agains, 1)] = begin + tid;
+        else l.item[atomicAdd(&l.items, 1)] = 2 * b.w1 + (b.w1 + (kLpUnroll - 1) * TH < end ? 0 : 1);
     }
     __syncthreads();
-    if (s_agains) {
-        const int full = (end - begin) / (TH * kLpUnroll), turns = full + kLpUnroll, all = s_agains * turns;      // each thread's, at most
+    if (l.agains) {                              // a warp for each, a word a lane
 #pragma unroll 1
-        for (int i = tid; i < all; i += TH) {
-            const int t = i % turns, first = s_again[i / turns];
-            const int own = end - first < TH * (kLpUnroll - 1) + 1 ? 0 : (end - first - TH * (kLpUnroll - 1) - 1) / (TH * kLpUnroll) + 1;
-            const int w = first + (t < own ? t * kLpUnroll : own * kLpUnroll + t - own) * TH;
-            if (w < end) offer(r, w, end, floor_key, floor_v, l);
-        }
+        for (int i = tid >> 5; i < l.agains; i += TH / 32)
+#pragma unroll 1
+            for (int w = l.again[i] + lane * TH; w < end; w += 32 * TH)
+                if (in(vec_max<T>(r.load(w)), w)) {
+                    const int to = atomicAdd(&l.items, 1);
+                    if (to < l.ITEMS) l.item[to] = 2 * w + 1;
+                }
         __syncthreads();
     }
-    const int n = l.count;
+    const int given = l.items, all = given < l.ITEMS ? given : l.ITEMS, items = all + (edges ? 1 : 0);
+#pragma unroll 1
+    for (int i = tid >> 5; i < items; i += TH / 32) {
+        const bool edge = i == all;
+        static_assert(kLpUnroll * VE <= 32 && Row<T>::EDGES <= 32, "an item's elements are a warp's lanes");
+        const int what = edge ? 0 : l.item[i];
+        int index = lane < ((what & 1) ? VE : kLpUnroll * VE) ? r.index((what >> 1) + lane / VE * TH) + lane % VE : -1;
+        if (edge) index = lane < Row<T>::EDGES ? r.edge(lane) : -1;
+        unsigned long long key = 0;
+        if (index >= 0) {
+            const float x = to_f32(r.at(index));
+            if (x >= floor_v) key = top_key(x, index);
+        }
+        const uint32_t who = __ballot_sync(0xffffffffu, key && key >= floor_key);
+        if (!who) continue;
+        int to = 0;
+        if (lane == 0) to = atomicAdd(&l.count, __popc(who));
+        to = __shfl_sync(0xffffffffu, to, 0) + __popc(who & ((1u << lane) - 1));
+        if (((who >> lane) & 1u) && to < TopList<TH>::CAP) l.key[to] = key;
+    }
     __syncthreads();
-    return n;
+    const int n = l.count, least = given > l.ITEMS ? TopList<TH>::CAP + 1 : 0;
+    __syncthreads();
+    return n > least ? n : least;
 }
-// The k-th largest of the threads' best keys, a floor that values tied in many places do not reach (0: fewer than k threads met a number).
+// A floor that values tied in many places do not reach: the k-th largest of the threads' best values, each with the last position of the
+// first word that holds it (0: fewer than k threads met a number).
 template <typename T, int TH>
 __device__ __noinline__ unsigned long long exact_floor(const Row<T> r, int end, const Best b, int k, TopList<TH> &l) {
     __shared__ unsigned long long s_floor;
     unsigned long long mine = 0;
     if (b.w1 >= 0) {
-        uint4 v[kLpUnroll];
-        load_turn<T, TH>(r, b.w1, end, v);
-#pragma unroll
-        for (int u = 0; u < kLpUnroll; ++u) {
-            const unsigned long long key = word_best<T>(v[u], r.index(b.w1 + u * TH));
-            if (key > mine) mine = key;
-        }
+        int w = b.w1;
+#pragma unroll 1
+        while (w + TH < end && w < b.w1 + (kLpUnroll - 1) * TH && vec_max<T>(r.load(w)) != b.v1) w += TH;
+        mine = top_key(b.v1, r.index(w) + Row<T>::VE - 1);
     }
     l.key[threadIdx.x] = mine;
     if (threadIdx.x == 0) s_floor = 0;
     __syncthreads();
-    int larger = 0;
-#pragma unroll 4
-    for (int j = 0; j < TH; ++j) larger += l.key[j] > mine;
-    if (larger == k - 1 && mine) s_floor = mine;
+    if (mine && larger_keys(l, TH, mine) == k - 1) s_floor = mine;
     __syncthreads();
     return s_floor;
 }
@@ -251,7 +216,8 @@ __device__ __noinline__ void top_of_words(const Row<T> r, int begin, int end, bo
     while (n > TopList<TH>::CAP) {
         // Still more than there is room for (rows in an order made for it, rows of mostly NaN): again from the k-th best of those
         // that had room, a floor that all but k of them no longer reach.
-        top_cut(l, TopList<TH>::CAP, k);
+        // (a list that has no room for all words holds at least as many keys as words, but for one whose tie lies before the floor)
+        top_cut(l, l.count < TopList<TH>::CAP ? l.count : TopList<TH>::CAP, k);
         floor_key = l.key[k - 1];
         __syncthreads();
         n = collect<T, TH>(r, begin, end, edges, b, floor_key, l);
@@ -260,14 +226,15 @@ __device__ __noinline__ void top_of_words(const Row<T> r, int begin, int end, bo
 }
 
 // What the CTAs of a cluster hand to the first: (s, m), (length of the list, w), and the list.
-template <int K> struct TopIn { unsigned long long part[8][2], key[8][K]; };
+template <int K> struct TopIn { unsigned long long part[8][2], key[8][K]; };          // lists end in zeros
 
 template <typename T, bool TOP, int TH>
 __global__ void __launch_bounds__(TH, (TOP ? 1280 : 1536) / TH) logprobs_row_kernel(const LogprobArgs a) {
     constexpr int VE = Row<T>::VE, U = kLpUnroll, WARPS = TH / 32;
     __shared__ TopList<TH> s_top;
     __shared__ Stats s_warp[WARPS];
-    __shared__ TopIn<TOP ? kTopMax : 1> s_in;
+    extern __shared__ __align__(16) unsigned char s_dynamic[];
+    TopIn<TOP ? kTopMax : 1> &s_in = *reinterpret_cast<TopIn<TOP ? kTopMax : 1> *>(s_dynamic);      // in clusters
     const uint32_t rank = rows_cluster_rank(), share = rows_cluster_size();
     if (share > 1) rows_cluster_arrive();
     pdl_enter();
@@ -330,10 +297,11 @@ __global__ void __launch_bounds__(TH, (TOP ? 1280 : 1536) / TH) logprobs_row_ker
             st_peer_u64(&s_in.part[rank][0], 0, ((unsigned long long)__float_as_uint(st.s) << 32) | __float_as_uint(st.m));
             st_peer_u64(&s_in.part[rank][1], 0, ((unsigned long long)(TOP ? s_top.count : 0) << 32) | __float_as_uint(st.w));
         }
-        if (TOP && (int)threadIdx.x < s_top.count) st_peer_u64(&s_in.key[rank][threadIdx.x], 0, s_top.key[threadIdx.x]);
+        if (TOP && (int)threadIdx.x < a.k)
+            st_peer_u64(&s_in.key[rank][threadIdx.x], 0, (int)threadIdx.x < s_top.count ? s_top.key[threadIdx.x] : 0ull);
         rows_cluster_sync();
         if (rank != 0) return;
-        if (warp == 0) {
+        if (warp == WARPS - 1) {
             st.reset();
             if (lane < (int)share) {
                 st.m = __uint_as_float((uint32_t)s_in.part[lane][0]);
@@ -341,39 +309,43 @@ __global__ void __launch_bounds__(TH, (TOP ? 1280 : 1536) / TH) logprobs_row_ker
                 st.w = __uint_as_float((uint32_t)s_in.part[lane][1]);
             }
             warp_join(st, a.c);
-            if (lane == 0) s_warp[0] = st;
         }
         if (TOP) {
+            // a key's place: its own in its list, and in each other list the number of larger keys, all found side by side
+            int taken = 0;
             for (int i = threadIdx.x; i < (int)share * a.k; i += TH) {
                 const int list = i / a.k, j = i - list * a.k;
-                if (j >= (int)(s_in.part[list][1] >> 32)) continue;
                 const unsigned long long mine = s_in.key[list][j];
-                int ahead = j;
-                for (int o = 0; o < (int)share && ahead < a.k; ++o) {
-                    if (o == list) continue;
-                    int low = 0, high = (int)(s_in.part[o][1] >> 32);         // the number of larger keys
-                    while (low < high) {
-                        const int mid = (low + high) >> 1;
-                        if (s_in.key[o][mid] > mine) low = mid + 1;
-                        else high = mid;
+                int pos[8] = {};
+#pragma unroll 1
+                for (int step = kTopMax; step > 0; step >>= 1) {
+#pragma unroll
+                    for (int o = 0; o < 8; ++o) {
+                        const int to = pos[o] + step;
+                        const unsigned long long other = s_in.key[o][to < kTopMax ? to - 1 : kTopMax - 1];
+                        pos[o] = to <= a.k && other > mine ? to : pos[o];
                     }
-                    ahead += low;
                 }
-                if (ahead < a.k) s_top.key[ahead] = mine;
+                int ahead = j;
+#pragma unroll
+                for (int o = 0; o < 8; ++o) ahead += o < (int)share && o != list ? pos[o] : 0;
+                if (mine && ahead < a.k) { s_top.key[ahead] = mine; ++taken; }
             }
-            if (threadIdx.x == 0) {
-                int n = 0;
-                for (int o = 0; o < (int)share; ++o) n += (int)(s_in.part[o][1] >> 32);
-                s_top.count = n < a.k ? n : a.k;
-            }
+            if (threadIdx.x == 0) s_top.count = 0;
+            __syncthreads();
+            if (taken) atomicAdd(&s_top.count, taken);
         }
     }
+    // One warp answers; the last, which has joined the cluster's sums.
     __shared__ RowAnswer s_answer;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const RowAnswer ans(s_warp[0], a.inv_t);
-        s_answer = ans;
-        answer_row<T>(a, row, s_warp[0], ans);
+    if (share == 1) __syncthreads();
+    if (warp == WARPS - 1) {
+        if (share == 1) st = s_warp[0];
+        const RowAnswer ans(st, a.inv_t);
+        if (lane == 0) {
+            s_answer = ans;
+            answer_row<T>(a, row, st, ans);
+        }
     }
     if (TOP) {
         __syncthreads();
@@ -408,23 +380,45 @@ __global__ void __launch_bounds__(128) logprobs_warp_kernel(const LogprobArgs a)
     const RowAnswer ans(st, a.inv_t);
     if (lane == 0) answer_row<T>(a, row, st, ans);
     if (a.k == 0) return;
-    uint32_t taken = 0;
-    for (int j = 0; j < a.k; ++j) {
-        uint32_t best = 0;                       // order bits of a number are never 0 (that is a NaN's)
-        int at = 0;
+    // Each turn takes the warp's largest.  The values' order bits lie in shared memory (0: no number, or taken; a number's are never 0), a lane
+    // keeps the best of each group of eight of its own, and only the group that the taken one was in is looked through again.
+    constexpr int GROUP = E < 8 ? E : 8, GROUPS = E / GROUP;
+    __shared__ uint32_t s_order[4][E * 32];
+    uint32_t *mine = s_order[threadIdx.x >> 5] + lane, best[GROUPS];
+    int at[GROUPS];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const bool in = !((taken >> i) & 1u) && f[i] == f[i] && lane + 32 * i < a.V;
-            const uint32_t o = in ? order_bits(f[i]) : 0u;
-            if (o > best) { best = o; at = i; }
+    for (int i = 0; i < E; ++i) mine[32 * i] = f[i] == f[i] && lane + 32 * i < a.V ? order_bits(f[i]) : 0u;
+    auto look = [&](int g) {
+        uint32_t top = 0;
+        int where = g * GROUP;
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j) {
+            const uint32_t o = mine[32 * (g * GROUP + j)];
+            if (o > top) { top = o; where = g * GROUP + j; }
         }
-        const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-        const uint32_t index = __reduce_min_sync(0xffffffffu, best == top && top ? (uint32_t)(lane + 32 * at) : 0x7fffffffu);
-        if (top && index == (uint32_t)(lane + 32 * at) && best == top) taken |= 1u << at;
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q)
+            if (q == g) { best[q] = top; at[q] = where; }
+    };
+#pragma unroll 1
+    for (int g = 0; g < GROUPS; ++g) look(g);
+#pragma unroll 1
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t own = best[0];
+        int where = at[0];
+#pragma unroll
+        for (int q = 1; q < GROUPS; ++q)
+            if (best[q] > own) { own = best[q]; where = at[q]; }
+        const uint32_t top = __reduce_max_sync(0xffffffffu, own);
+        const uint32_t index = __reduce_min_sync(0xffffffffu, own == top && top ? (uint32_t)(lane + 32 * where) : 0x7fffffffu);
         if (lane == 0) {
             a.top_logprob[row * a.k + j] = top ? ans.of(from_order_bits(top)) : NAN;
             a.top_index[row * a.k + j] = top ? (int32_t)index : -1;
         }
+        if (!top) continue;
+        const int gone = (int)(index >> 5);
+        if (lane == (int)(index & 31)) mine[32 * gone] = 0;
+        look(gone / GROUP);
     }
 }
 
@@ -513,10 +507,11 @@ extern "C" lpdt_status lpdt_token_logprobs(int64_t rows, int32_t V, const void *
         } else {
             const int cs = row_share(rows, (int64_t)V * sizeof(T), 4, 4096);
             const unsigned grid = (unsigned)(rows * cs);
+            const size_t in = cs == 1 ? 0 : top_k ? sizeof(TopIn<kTopMax>) : sizeof(TopIn<1>);
             if ((int64_t)V * (int64_t)sizeof(T) / cs <= 16384)
-                launch_k_cluster(top_k ? logprobs_row_kernel<T, true, 128> : logprobs_row_kernel<T, false, 128>, grid, 128, 0, st, cs, a);
+                launch_k_cluster(top_k ? logprobs_row_kernel<T, true, 128> : logprobs_row_kernel<T, false, 128>, grid, 128, in, st, cs, a);
             else
-                launch_k_cluster(top_k ? logprobs_row_kernel<T, true, 256> : logprobs_row_kernel<T, false, 256>, grid, 256, 0, st, cs, a);
+                launch_k_cluster(top_k ? logprobs_row_kernel<T, true, 256> : logprobs_row_kernel<T, false, 256>, grid, 256, in, st, cs, a);
         }
         LPDT_LAUNCH_CHECK();
         return LPDT_OK;
