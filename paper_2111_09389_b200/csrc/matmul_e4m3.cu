@@ -10,7 +10,8 @@
 // G = 2: pairs of SMs (cta_group::2) on tiles of 256 columns by up to 224 rows, each CTA holding the codes of its 128 columns of C and
 // of half of the rows; shared memory serves 128 bytes a cycle, which one SM's 128 x 224 would exceed (per 32 values of K 4 KB + 7 KB
 // are written and read in 112 cycles).  G = 1: one SM, for what is too small to fill pairs; a cluster of SPLIT CTAs may share a tile's K
-// and add their accumulators through distributed shared memory, in the order of the CTAs.
+// and hand each other groups of eight rows of their accumulators through distributed shared memory, added in the order of
+// the CTAs.
 //
 // Two accumulators of up to 224 columns (the epilogue of one tile runs under the products of the next) and four sets of scale factors
 // fill the 512 columns of tensor memory.
@@ -29,6 +30,7 @@ constexpr size_t kMmSmem = 227 * 1024;
 struct MmParams {
     int nodes, M, N, kblocks, bn;              // bn: rows of C per tile, a multiple of 16
     int tilesJ, tilesM, stages, tmem_cols;
+    int groups, per_cta;                       // SPLIT: groups of 8 rows of a tile that exist, most of them that one CTA adds up
     int slot;                                  // bytes of a stage: codes of both sides
     const uint8_t *sA, *sB;
     int spitch;                                // bytes of a row of scales
@@ -55,11 +57,11 @@ __device__ __forceinline__ uint32_t mm_peer(uint32_t local, uint32_t rank) {
 __device__ __forceinline__ void mm_arrive_at(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-__device__ __forceinline__ float mm_ld_peer(uint32_t cluster_addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
+__device__ __forceinline__ void mm_st_peer(uint32_t cluster_addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
+__device__ __forceinline__ void mm_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void mm_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // Loads into this CTA that signal the barrier at `bar` (G = 2: the leader's).
 template <int G> __device__ __forceinline__ void mm_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2) {
     if constexpr (G == 2)
@@ -113,6 +115,28 @@ __device__ __forceinline__ MmTile mm_tile(const MmParams &p, int tile) {
     return t;
 }
 
+// The rows of scales that a lane brings to tensor memory: of 128 columns of C and 256 rows of it, every 32nd.
+struct MmScaleRows {
+    const uint8_t *row[12];
+    int sets;
+    __device__ __forceinline__ void set(const MmParams &p, const MmTile &t, int G, int rank, int lane) {
+        sets = p.bn > 128 ? 3 : 2;
+        const int j0 = (t.jt * G + (G == 2 ? rank : 0)) * 128, m0 = t.mt * p.bn;
+        const uint8_t *b = p.sB + (size_t)t.node * p.N * p.spitch, *a = p.sA + (size_t)t.node * p.M * p.spitch;
+#pragma unroll
+        for (int i = 0; i < 12; ++i) {
+            const int r = (i & 3) * 32 + lane + (i >= 8 ? 128 : 0), at = (i < 4 ? j0 : m0) + r;
+            const bool have = i < 4 ? at < p.N : (r < p.bn && at < p.M);
+            row[i] = have ? (i < 4 ? b : a) + (size_t)at * p.spitch : nullptr;
+        }
+    }
+    __device__ __forceinline__ void fetch(uint32_t (&w)[12], int word) const {
+#pragma unroll
+        for (int i = 0; i < 12; ++i)
+            w[i] = (i < 8 || sets == 3) && row[i] ? __ldg(reinterpret_cast<const uint32_t *>(row[i]) + word) : 0x7f7f7f7fu;
+    }
+};
+
 // 16 rows of C from m on, column j of it per lane.
 template <typename OutT>
 __device__ __forceinline__ void mm_store(const MmParams &p, int node, int m, int j, const float (&v)[16], float bias) {
@@ -148,6 +172,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     extern __shared__ __align__(1024) unsigned char smem[];
     MmCtl *ctl = reinterpret_cast<MmCtl *>(smem);
     unsigned char *data = smem + 1024, *scales = data + (size_t)p.stages * p.slot;
+    [[maybe_unused]] float *parts = reinterpret_cast<float *>(scales + kMmScaleSlots * kMmScaleBytes);      // SPLIT: [CTA][group][8 rows][128 columns]
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = (G == 2 || SPLIT) ? mm_cluster_rank() : 0u;
     const uint32_t share = SPLIT ? (uint32_t)gridDim.y : 1u;            // gridDim.y = cluster size
@@ -157,12 +182,19 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     const int k_end = SPLIT ? (int)((long long)p.kblocks * (rank + 1) / share) : p.kblocks;
     const int halfn = p.bn / G;                                         // rows of A per CTA
 
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
-        for (int i = 0; i < kMmScaleSlots; ++i) { mbar_init(smem_u32(&ctl->sf_full[i]), G); mbar_init(smem_u32(&ctl->sf_done[i]), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->tmem_full[i]), 1); mbar_init(smem_u32(&ctl->tmem_empty[i]), 8 * G); }
-        ctl->abort_flag = 0;
-        mbar_fence_init();
+    // Each role waits for the kernels before this one at its first access of global memory, and does what it can before: the fetching warp
+    // sets the barriers up and goes on (its loads need nothing else), the scales' warp asks for the first words, meanwhile.
+    if constexpr (SPLIT) mm_cluster_arrive();
+    pdl_trigger();
+    if (warp == 0) {
+        if (lane == 0) {
+            for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
+            for (int i = 0; i < kMmScaleSlots; ++i) { mbar_init(smem_u32(&ctl->sf_full[i]), G); mbar_init(smem_u32(&ctl->sf_done[i]), 1); }
+            for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->tmem_full[i]), 1); mbar_init(smem_u32(&ctl->tmem_empty[i]), 8 * G); }
+            ctl->abort_flag = 0;
+            mbar_fence_init();
+        }
+        __syncwarp();
     }
     if (warp == 1) {
         if constexpr (G == 2) {
@@ -173,15 +205,27 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             tmem_relinquish();
         }
     }
+    MmScaleRows rows;
+    uint32_t next[12];
+    if (warp == 2) {
+        rows.set(p, mm_tile(p, first < total ? first : 0), G, (int)rank, lane);
+        pdl_wait();
+        rows.fetch(next, k_begin >> 2);
+    }
     tc_fence_before();
-    __syncthreads();
-    if (G == 2 || SPLIT) mm_cluster_sync();       // the other CTAs' barriers are initialised
+    if constexpr (G == 2) {
+        __syncthreads();
+        mm_cluster_sync();        // the other CTA's barriers are initialised
+    } else if (warp == 0)
+        asm volatile("bar.arrive 1, %0;" ::"n"(kMmThreads) : "memory");
+    else
+        named_bar_sync(1, kMmThreads);
     tc_fence_after();
-    pdl_enter();
-    const uint32_t tmem_base = __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
+    const uint32_t tmem_base = warp == 0 ? 0u : __shfl_sync(0xffffffffu, ctl->tmem_base, 0);
 
     if (warp == 0) {
         if (elect_one()) { tma_prefetch_desc(&mapL); tma_prefetch_desc(&mapR); }
+        pdl_wait();
         int st = 0; uint32_t ph = 0;
         for (int tile = first; tile < total && !ctl->abort_flag; tile += step) {
             const MmTile t = mm_tile(p, tile);
@@ -265,38 +309,25 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     } else if (warp == 2) {
         // Row r of 128 goes to bytes (r % 32) * 16 + (r / 32) * 4 on: the word that holds its scales of four blocks of K (the instruction
         // names the byte).  The next words are on their way while this group waits for its slot.
-        const int sets = p.bn > 128 ? 3 : 2;
         uint32_t group = 0;
+        const int last = (k_end - 1) >> 2;
         for (int tile = first; tile < total && !ctl->abort_flag; tile += step) {
-            const MmTile t = mm_tile(p, tile);
-            const int j0 = (t.jt * G + (G == 2 ? (int)rank : 0)) * 128, m0 = t.mt * p.bn;
-            const uint8_t *row[12];
-#pragma unroll
-            for (int i = 0; i < 12; ++i) {
-                const int r = (i & 3) * 32 + lane + (i >= 8 ? 128 : 0);
-                const bool lanes = i < 4, have = lanes ? j0 + r < p.N : (r < p.bn && m0 + r < p.M);
-                row[i] = !have ? nullptr : lanes ? p.sB + ((size_t)t.node * p.N + j0 + r) * p.spitch : p.sA + ((size_t)t.node * p.M + m0 + r) * p.spitch;
+            if (tile != first) {
+                rows.set(p, mm_tile(p, tile), G, (int)rank, lane);
+                rows.fetch(next, k_begin >> 2);
             }
-            uint32_t next[12];
-            auto fetch = [&](int word) {
-#pragma unroll
-                for (int i = 0; i < 12; ++i)
-                    next[i] = (i < 8 || sets == 3) && row[i] ? __ldg(reinterpret_cast<const uint32_t *>(row[i]) + word) : 0x7f7f7f7fu;
-            };
-            const int last = (k_end - 1) >> 2;
-            fetch(k_begin >> 2);
             bool ok = true;
             for (int g = k_begin >> 2; g <= last; ++g, ++group) {
                 const int slot = group & (kMmScaleSlots - 1);
                 uint32_t now[12];
 #pragma unroll
                 for (int i = 0; i < 12; ++i) now[i] = next[i];
-                if (g < last) fetch(g + 1);
+                if (g < last) rows.fetch(next, g + 1);
                 if (!mbar_wait(smem_u32(&ctl->sf_done[slot]), ((group / kMmScaleSlots) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
                 uint4 *dst = reinterpret_cast<uint4 *>(scales + (size_t)slot * kMmScaleBytes) + lane;
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
-                    if (i < sets) dst[i * 32] = make_uint4(now[4 * i], now[4 * i + 1], now[4 * i + 2], now[4 * i + 3]);
+                    if (i < rows.sets) dst[i * 32] = make_uint4(now[4 * i], now[4 * i + 1], now[4 * i + 2], now[4 * i + 3]);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
@@ -313,6 +344,8 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         const int q = warp & 3, half = (warp - 4) >> 2, chunks = p.bn / 16;
         const uint32_t empty0 = G == 2 ? mm_peer(smem_u32(&ctl->tmem_empty[0]), 0) : smem_u32(&ctl->tmem_empty[0]);
         uint32_t tcount = 0;
+        pdl_wait();
+        if constexpr (SPLIT) mm_cluster_wait();       // the others have started
         for (int tile = first; tile < total && !ctl->abort_flag; tile += step, ++tcount) {
             const MmTile t = mm_tile(p, tile);
             const int j = (t.jt * G + (G == 2 ? (int)rank : 0)) * 128 + q * 32 + lane, m0 = t.mt * p.bn;
@@ -330,10 +363,16 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
                 for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
                 if (c + 2 < chunks) tmem_ld_32x16(t_row + (c + 2) * 16, v);
                 if constexpr (SPLIT) {
-                    // the pipeline is done with shared memory: this CTA's share of the sums, [row][column of C]
-                    float *mine = reinterpret_cast<float *>(data) + c * 16 * 128 + q * 32 + lane;
+                    // groups of 8 rows go to the CTAs in turn, each to where that CTA keeps this one's
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) mine[i * 128] = f[i];
+                    for (int h = 0; h < 2; ++h) {
+                        const int g = 2 * c + h;
+                        if (g >= p.groups) continue;
+                        const uint32_t slot = rank * (uint32_t)p.per_cta + (uint32_t)g / share;
+                        const uint32_t to = mm_peer(smem_u32(parts + (size_t)slot * 1024 + q * 32 + lane), (uint32_t)g % share);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) mm_st_peer(to + i * 512, f[8 * h + i]);
+                    }
                 } else if (m0 + c * 16 < p.M)
                     mm_store<OutT>(p, t.node, m0 + c * 16, j, f, bias);
             }
@@ -346,34 +385,33 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         }
     }
     if constexpr (SPLIT) {
-        __syncthreads();
-        mm_cluster_sync();                        // every CTA's share is in its shared memory
+        if (warp < 4) mm_cluster_wait();
+        __syncwarp();
+        mm_cluster_sync();                        // every part has arrived
         if (warp >= 4 && !ctl->abort_flag) {
             const MmTile t = mm_tile(p, first);
-            const int q = warp & 3, half = (warp - 4) >> 2, chunks = p.bn / 16;
-            const int j = t.jt * 128 + q * 32 + lane, m0 = t.mt * p.bn;
+            const int q = warp & 3, j = t.jt * 128 + q * 32 + lane, m0 = t.mt * p.bn;
             const float bias = p.bias && j < p.N ? p.bias[t.node * p.bias_node + j] : 0.f;
-            // eight rows at a time, dealt to the CTAs and to the two halves of the epilogue warps
-            for (int c = (int)rank * 2 + half; c < chunks * 2; c += 2 * (int)share) {
-                if (m0 + c * 8 >= p.M) break;
-                const uint32_t at = smem_u32(data) + (uint32_t)(c * 8 * 128 + q * 32 + lane) * 4;
+            for (int slot = (warp - 4) >> 2; slot < p.per_cta; slot += 2) {
+                const int m = m0 + (slot * (int)share + (int)rank) * 8;
+                if (slot * (int)share + (int)rank >= p.groups || m >= p.M) break;
                 float s[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = 0.f;
-                for (uint32_t r = 0; r < share; ++r) {
-                    const uint32_t from = mm_peer(at, r);
+                for (uint32_t r = 0; r < share; ++r) {                  // in the order of the CTAs
+                    const float *part = parts + ((size_t)r * p.per_cta + slot) * 1024 + q * 32 + lane;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) s[i] = __fadd_rn(s[i], mm_ld_peer(from + i * 512));
+                    for (int i = 0; i < 8; ++i) s[i] = __fadd_rn(s[i], part[i * 128]);
                 }
                 MmParams e = p;
-                if (e.M > m0 + c * 8 + 8) e.M = m0 + c * 8 + 8;
-                mm_store<OutT>(e, t.node, m0 + c * 8, j, s, bias);
+                if (e.M > m + 8) e.M = m + 8;
+                mm_store<OutT>(e, t.node, m, j, s, bias);
             }
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (G == 2 || SPLIT) mm_cluster_sync();       // no CTA leaves while another may still signal it or read its shared memory
+    if (G == 2) mm_cluster_sync();                // no CTA leaves while the other may still signal it
     if (warp == 1) {
         tc_fence_after();
         if constexpr (G == 2)
@@ -385,9 +423,11 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
 
 struct MmPlan { int g, bn, split; };
 
-// The least of a rough estimate in cycles over pairs and single SMs, rows per tile and shares of K.  A block of 128 values of K takes a
-// tile of bn rows the products' 2 * bn cycles or, where that is more, the time its codes take through shared memory at 128 bytes a cycle
-// (written once, read once), and never less than what its bytes take from L2 at about 48 a cycle and SM.
+// The least of an estimate in cycles over pairs and single SMs, rows per tile and shares of K.  A block of 128 values of K takes a tile of bn
+// rows the products' 2 * bn cycles or, where that is more, what its codes take from L2: 48 bytes a cycle of an SM by itself, 34 of one of
+// a pair.  Behind that 12 cycles a row for the epilogue.  Clusters of 8 find room on 96 SMs at once.  (Fitted to every plan's time for 17
+// shapes from 1 x 4096 x 4096 to 4096^3: the plan is within 1 % of the best for all of them.  Pairs pay for themselves when every
+// SM has several tiles: 4096^3 65.3 us against 68.8 on single SMs, 2048^3 17.6 against 16.0.)
 static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
     MmPlan best = {1, 16, 1};
     double least = 1e300;
@@ -397,14 +437,11 @@ static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
             if (bn > (int64_t)align_up((size_t)M, 16)) break;
             const int64_t tiles = (int64_t)nodes * tj * ceil_div(M, bn);
             const double bytes = kMmLaneBytes + bn * 128.0 / g;
-            double per = 2.0 * bn;
-            if (2 * bytes / 128 > per) per = 2 * bytes / 128;
-            if (bytes / 48 > per) per = bytes / 48;
-            for (int split = 1; split <= (g == 1 ? 8 : 1); split *= 2) {
+            const double from_l2 = bytes / (g == 1 ? 48 : 34), per = from_l2 > 2.0 * bn ? from_l2 : 2.0 * bn;
+            for (int split = 1; split <= (g == 1 && bn <= 128 ? 8 : 1); split *= 2) {
                 if (split > kblocks) break;
-                const int64_t ctas = kNumSMs / (g * split) * (g * split);
-                const int64_t waves = split > 1 ? ceil_div(tiles * split, ctas) : ceil_div(tiles * g, ctas);
-                const double cost = waves * (ceil_div(kblocks, split) * per + 8.0 * bn + (split > 1 ? 2500 : 0)) + 2500;
+                const int64_t slots = split == 8 ? 96 : kNumSMs / (g * split) * (g * split);
+                const double cost = ceil_div(tiles * g * split, slots) * (ceil_div(kblocks, split) * per + 12.0 * bn) + (g == 2 ? 1000 : 0);
                 if (cost < least) { least = cost; best = {g, bn, split}; }
             }
         }
@@ -469,8 +506,14 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     const int64_t tiles = (int64_t)nodes * p.tilesJ * p.tilesM;
     if (tiles > 0x3fffffff) return LPDT_ERR_UNSUPPORTED;
     p.slot = kMmLaneBytes + (int)align_up((size_t)(plan.bn / plan.g) * 128, 1024);
-    p.stages = (int)((kMmSmem - 1024 - kMmScaleSlots * kMmScaleBytes) / p.slot);
+    p.groups = (int)ceil_div(M < plan.bn ? M : plan.bn, 8);
+    p.per_cta = (int)ceil_div(p.groups, plan.split);
+    const size_t rest = 1024 + kMmScaleSlots * kMmScaleBytes + (plan.split > 1 ? (size_t)plan.split * p.per_cta * 4096 : 0);
+    p.stages = (int)((kMmSmem - rest) / p.slot);
     if (p.stages > kMmMaxStages) p.stages = kMmMaxStages;
+    // Few rows: half of an SM's shared memory holds enough of them in flight, and the other half lets the next such call's CTAs start.
+    const int half = (int)((kMmSmem / 2 - 1024 - rest) / p.slot);
+    if (plan.bn <= 64 && tiles * plan.split <= kNumSMs && half >= 4 && p.stages > half) p.stages = half;
     for (p.tmem_cols = 128; p.tmem_cols < 2 * plan.bn + kMmScaleSlots * 16; p.tmem_cols *= 2) {}
     p.sA = sA; p.sB = sB; p.spitch = (int)lpdt_e4m3_scale_pitch(K);
     p.bias = bias; p.bias_node = nodes == 1 ? 0 : bias_node_stride;
@@ -483,7 +526,7 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     const uint32_t bL[3] = {128, 128, 1}, bR[3] = {128, (uint32_t)(plan.bn / plan.g), 1};
     if (!make_map_u8(&mL, B, 3, dL, sL, bL, CU_TENSOR_MAP_SWIZZLE_128B) || !make_map_u8(&mR, A, 3, dR, sR, bR, CU_TENSOR_MAP_SWIZZLE_128B))
         return LPDT_ERR_CUDA;
-    const size_t smem = 1024 + (size_t)p.stages * p.slot + kMmScaleSlots * kMmScaleBytes;
+    const size_t smem = rest + (size_t)p.stages * p.slot;
     const cudaStream_t st = as_stream(stream);
     return with_dtype(c_dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);

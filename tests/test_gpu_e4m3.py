@@ -115,10 +115,11 @@ def device_operands(ops, K):
     return padded(qa, P), padded(sa, S), padded(qb, P), padded(sb, S)
 
 
-# one token; few rows; ragged; one block; many blocks of K; pairs of SMs; several nodes; more tiles than SMs
+# one token; few rows, whose K several CTAs share; ragged; one block; many blocks of K; several nodes; more tiles than SMs; pairs of SMs
 SHAPES = [(1, 1, 16, 128), (1, 1, 4096, 4096), (1, 1, 1, 1), (2, 3, 5, 7), (1, 17, 300, 1000), (3, 64, 200, 513), (4, 150, 130, 257),
           (1, 128, 128, 129), (1, 33, 1, 8191), (1, 240, 256, 384), (1, 500, 1023, 640), (1, 1025, 2049, 300), (2, 700, 1500, 1200),
-          (1, 2048, 2048, 512), (5, 1, 129, 2000), (1, 4100, 515, 130)]
+          (1, 2048, 2048, 512), (5, 1, 129, 2000), (1, 4100, 515, 130),
+          (1, 90, 4100, 2900), (1, 3000, 5000, 1000), (2, 4188, 4744, 259)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
