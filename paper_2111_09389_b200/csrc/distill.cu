@@ -147,11 +147,11 @@ __device__ __forceinline__ Stats unpack_sums(unsigned long long v) {
 // needed in L2, which leaves it to the words that wait for theirs.  (Tried instead and slower: words held in shared memory between the passes
 // by CTAs that walk over rows, 612 us for 4096 x 131072 bf16 against 456, the exponentials of the two passes no longer side by side.)
 template <typename T, int TH>
-__global__ void __launch_bounds__(TH, TH == 512 ? 2 : TH == 256 ? 5 : 10) distill_row_kernel(const DistillArgs a) {
-    constexpr int VE = Row<T>::VE, U = kDtUnroll, WARPS = TH / 32;
+__global__ void __launch_bounds__(TH + 32, TH == 512 ? 2 : TH == 256 ? 4 : 8) distill_row_kernel(const DistillArgs a) {
+    constexpr int VE = Row<T>::VE, U = kDtUnroll, WARPS = TH / 32, PER = kListMax / 32;
     extern __shared__ uint32_t s_bits[];              // a bit per element of this CTA's words: listed
     __shared__ List<kListMax> s_list;
-    __shared__ unsigned long long s_warp[WARPS], s_list_warp[WARPS], s_in[8], s_list_in[8];
+    __shared__ unsigned long long s_warp[WARPS], s_listed, s_in[8], s_list_in[8];
     const uint32_t rank = rows_cluster_rank(), share = rows_cluster_size();
     if (share > 1) rows_cluster_arrive();
     pdl_enter();
@@ -160,56 +160,106 @@ __global__ void __launch_bounds__(TH, TH == 512 ? 2 : TH == 256 ? 5 : 10) distil
     T *dx = a.dx ? (T *)a.dx + row * a.dx_row : nullptr;
     const bool same = ((uintptr_t)(dx + r.head) & 15) == 0;
     const int begin = (int)((long long)r.words * rank / share), end = (int)((long long)r.words * (rank + 1) / share);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int id = (int)threadIdx.x < a.k ? a.index[row * a.k + threadIdx.x] : -1;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool lister = warp == WARPS;                // the last warp sees to the list, the others to the row
     const float weight = a.weight ? a.weight[row] : 1.f;
     const double g = (double)weight * a.inv_t / (double)a.B;
-    const bool skip = weight == 0.f;                  // the same for the whole cluster
-    const int edge = rank == 0 && threadIdx.x < Row<T>::EDGES ? r.edge(threadIdx.x) : -1;
+    const int edge = rank == 0 && tid < Row<T>::EDGES ? r.edge(tid) : -1;
     float at_edge = -INFINITY;
-    bool mine = false, twice = false;                 // this thread's entry is the one that stands for its token here; some token has several
+    // the first turn is asked for before anything else (also of a row of weight 0, which needs none of it)
+    const int w0 = begin + tid;
+    const bool full = !lister && w0 + (U - 1) * TH < end;
+    uint4 ahead[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) ahead[u] = full ? r.load(w0 + u * TH) : make_uint4(0, 0, 0, 0);
+    auto put = [&](int w, const float *f, uint32_t out) {
+        T *to = dx + r.index(w);
+        if (same && !out) __stcs(reinterpret_cast<uint4 *>(to), pack_vec<T>(f));
+        else {
+#pragma unroll
+            for (int i = 0; i < VE; ++i)
+                if (!((out >> i) & 1u)) to[i] = from_f32<T>(f[i]);
+        }
+    };
+
+    if (weight == 0.f) {                              // the same for the whole cluster
+        if (share > 1) { rows_cluster_wait(); rows_cluster_sync(); }
+        if (rank == 0 && tid == 0) a.row_loss[row] = 0.f;
+        if (!dx) return;
+        const float zeros[VE] = {};
+        for (int w = w0; w < end && !lister; w += TH) put(w, zeros, 0);
+        if (edge >= 0) dx[edge] = from_f32<T>(0.f);
+        return;
+    }
+
     Stats st, sl;
     st.reset();
     sl.reset();
-    RowTerms terms = {};
-
-    if (!skip) {
-        // The bits need the list's positions alone; what the teacher says of them is made ready by the first warp while the others read.
+    int id[PER];
+    uint32_t mine = 0;                                // the lister's: entry lane + 32 i is the one that stands for its token here
+    bool again = false;                               // some token has several entries
+    if (lister) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = lane + 32 * i;
+            id[i] = j < a.k ? a.index[row * a.k + j] : -1;
+            if (id[i] >= a.V) {
+                if (rank == 0 && a.dev_status) atomicCAS(a.dev_status, 0, (int32_t)LPDT_ERR_INVALID_ARG);
+                id[i] = -1;
+            }
+            if (j < a.k) s_list.id[j] = id[i] < 0 ? -1 : id[i];
+        }
+    } else {
         const int bit_words = ((end - begin) * VE + 31) / 32;
-        for (int i = threadIdx.x; i < bit_words; i += TH) s_bits[i] = 0;
-        if ((int)threadIdx.x < a.k) s_list.id[threadIdx.x] = id >= 0 && id < a.V ? id : -1;
-        __syncthreads();
-        bool again = false;
-        if (id >= 0 && id < a.V) {
-            const int at = id - r.index(begin);
+        for (int i = tid; i < bit_words; i += TH) s_bits[i] = 0;
+    }
+    __syncthreads();
+    if (lister) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (id[i] < 0) continue;
+            const int at = id[i] - r.index(begin);
+            bool seen = false, here = true;
             if (at >= 0 && at < (end - begin) * VE) {
                 const uint32_t bit = 1u << (at & 31);
-                again = atomicOr(&s_bits[at >> 5], bit) & bit;
-                mine = !again;
-            } else if (rank == 0 && (id < r.head || id >= r.index(r.words))) {
-                for (int i = 0; i < (int)threadIdx.x; ++i) again |= s_list.id[i] == id;      // on the edges: few, so by looking
-                mine = !again;
+                seen = atomicOr(&s_bits[at >> 5], bit) & bit;
+            } else if (rank == 0 && (id[i] < r.head || id[i] >= r.index(r.words))) {
+                for (int j = 0; j < lane + 32 * i; ++j) seen |= s_list.id[j] == id[i];       // on the edges: few, so by looking
+            } else
+                here = false;
+            again |= here && seen;
+            if (here && !seen) mine |= 1u << i;
+        }
+    }
+    const bool twice = __syncthreads_or(again);
+    const uint8_t *bytes = reinterpret_cast<const uint8_t *>(s_bits);
+    auto listed = [&](int w) -> uint32_t {            // the bits of word w
+        const int i = w - begin;
+        return VE == 8 ? bytes[i] : (bytes[i >> 1] >> (4 * (i & 1))) & 15u;
+    };
+    if (lister) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = lane + 32 * i;
+            if (j >= a.k) continue;
+            const float x = id[i] >= 0 ? to_f32(r.at(id[i])) : -INFINITY;
+            s_list.x[j] = x;
+            s_list.logt[j] = id[i] >= 0 ? (double)a.value[row * a.k + j] : -INFINITY;
+            if ((mine >> i) & 1u) {
+                const float y[2] = {x, -INFINITY};
+                if (x > sl.m) sl.raise(x, a.c);
+                accumulate<2, false>(sl, y, a.c);
             }
         }
-        if (edge >= 0) {
-            at_edge = to_f32(r.at(edge));
-            bool out = false;
-            for (int j = 0; j < a.k; ++j) out |= s_list.id[j] == edge;
-            const float x[2] = {out ? -INFINITY : at_edge, -INFINITY};
-            if (x[0] > st.m) st.m = x[0];
-            accumulate<2, false>(st, x, a.c);
-        }
-        twice = __syncthreads_or(again);
-        if (mine) {
-            const float x[2] = {to_f32(r.at(id)), -INFINITY};
-            if (x[0] > sl.m) sl.m = x[0];
-            accumulate<2, false>(sl, x, a.c);
-        }
-        const uint8_t *bytes = reinterpret_cast<const uint8_t *>(s_bits);
-        auto word = [&](const uint4 &v, int i0) {
+        __syncwarp();
+        finish_list(a, s_list, lane);
+        warp_join(sl, a.c);
+        if (lane == 0) s_listed = pack_sums(sl);
+    } else {
+        auto word = [&](const uint4 &v, int w) {
             float f[VE];
             unpack_vec<T>(v, f);
-            const uint32_t out = VE == 8 ? bytes[i0] : (bytes[i0 >> 1] >> (4 * (i0 & 1))) & 15u;
+            const uint32_t out = listed(w);
             if (out) {
 #pragma unroll
                 for (int i = 0; i < VE; ++i) if ((out >> i) & 1u) f[i] = -INFINITY;
@@ -220,86 +270,88 @@ __global__ void __launch_bounds__(TH, TH == 512 ? 2 : TH == 256 ? 5 : 10) distil
             if (m > st.m) st.raise(m, a.c);
             accumulate<VE, false>(st, f, a.c);
         };
-        int w = begin + (int)threadIdx.x;
+        int w = w0;
+        if (full) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) word(ahead[u], w + u * TH);
+            w += U * TH;
+        }
         for (; w + (U - 1) * TH < end; w += TH * U) {
             uint4 v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u] = r.load(w + u * TH);
 #pragma unroll
-            for (int u = 0; u < U; ++u) word(v[u], w + u * TH - begin);
-        }
-        for (; w < end; w += TH) word(r.load(w), w - begin);
-        if (warp == 0) make_list<T>(a, row, s_list, lane, rank == 0);
-        warp_join(st, a.c);
-        warp_join(sl, a.c);
-        if (lane == 0) { s_warp[warp] = pack_sums(st); s_list_warp[warp] = pack_sums(sl); }
-        __syncthreads();
-        // each warp joins the warps' sums for itself, which saves a barrier
-        st.reset();
-        sl.reset();
-        if (lane < WARPS) { st = unpack_sums(s_warp[lane]); sl = unpack_sums(s_list_warp[lane]); }
-        warp_join(st, a.c);
-        warp_join(sl, a.c);
-        if (share > 1) {
-            // every CTA hands its sums to all
-            rows_cluster_wait();                      // they have started
-            if (warp == 0 && lane < (int)share) {
-                st_peer_u64(&s_in[rank], lane, pack_sums(st));
-                st_peer_u64(&s_list_in[rank], lane, pack_sums(sl));
-            }
-            // every CTA of the cluster has read what it gathers before any writes a gradient, which may lie where the logits do
-            rows_cluster_sync();
-            st.reset();
-            sl.reset();
-            if (lane < (int)share) { st = unpack_sums(s_in[lane]); sl = unpack_sums(s_list_in[lane]); }
-            warp_join(st, a.c);
-            warp_join(sl, a.c);
-        }
-        terms = row_terms(a, s_list.sum, st, sl, g);
-    } else {
-        if (share > 1) {
-            rows_cluster_wait();
-            rows_cluster_sync();
-        }
-    }
-    if (rank == 0 && warp == WARPS - 1) {
-        const double loss = skip ? 0.0 : row_loss(a, s_list, terms, st, lane);
-        if (lane == 0) a.row_loss[row] = (float)loss;
-    }
-    if (!dx) return;
-    auto grad = [&](float x) { return terms.rest * ex2(max_nan((x - st.m) * a.c, kFar)); };
-    auto put = [&](int w, const float *f) {
-        if (same) __stcs(reinterpret_cast<uint4 *>(dx + r.index(w)), pack_vec<T>(f));
-        else {
-#pragma unroll
-            for (int i = 0; i < VE; ++i) dx[r.index(w) + i] = from_f32<T>(f[i]);
-        }
-    };
-    int w = begin + (int)threadIdx.x;
-    if (!skip) {
-        auto word = [&](const uint4 &v, int at) {
-            float f[VE];
-            unpack_vec<T>(v, f);
-#pragma unroll
-            for (int i = 0; i < VE; ++i) f[i] = grad(f[i]);
-            put(at, f);
-        };
-        for (; w + (U - 1) * TH < end; w += TH * U) {
-            uint4 v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = r.load_last(w + u * TH);
-#pragma unroll
             for (int u = 0; u < U; ++u) word(v[u], w + u * TH);
         }
         for (; w < end; w += TH) word(r.load(w), w);
-    } else {
-        const float zeros[VE] = {};
-        for (; w < end; w += TH) put(w, zeros);
+        if (edge >= 0) {
+            at_edge = to_f32(r.at(edge));
+            bool out = false;
+            for (int j = 0; j < a.k; ++j) out |= s_list.id[j] == edge;
+            const float x[2] = {out ? -INFINITY : at_edge, -INFINITY};
+            if (x[0] > st.m) st.raise(x[0], a.c);
+            accumulate<2, false>(st, x, a.c);
+        }
+        warp_join(st, a.c);
+        if (lane == 0) s_warp[warp] = pack_sums(st);
     }
-    if (edge >= 0) dx[edge] = from_f32<T>(skip ? 0.f : grad(at_edge));
-    if (skip) return;
     __syncthreads();
-    if (mine) dx[s_list.id[threadIdx.x]] = from_f32<T>(listed_grad(a, s_list, terms, g, threadIdx.x, twice));
+    // each warp joins the warps' sums for itself, which saves a barrier
+    st.reset();
+    if (lane < WARPS) st = unpack_sums(s_warp[lane]);
+    warp_join(st, a.c);
+    sl = unpack_sums(s_listed);
+    if (share > 1) {
+        // every CTA hands its sums to all
+        rows_cluster_wait();                          // they have started
+        if (warp == 0 && lane < (int)share) {
+            st_peer_u64(&s_in[rank], lane, pack_sums(st));
+            st_peer_u64(&s_list_in[rank], lane, pack_sums(sl));
+        }
+        // every CTA of the cluster has read what it gathers before any writes a gradient, which may lie where the logits do
+        rows_cluster_sync();
+        st.reset();
+        sl.reset();
+        if (lane < (int)share) { st = unpack_sums(s_in[lane]); sl = unpack_sums(s_list_in[lane]); }
+        warp_join(st, a.c);
+        warp_join(sl, a.c);
+    }
+    const RowTerms terms = row_terms(a, s_list.sum, st, sl, g);
+    if (lister) {
+        if (dx) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if ((mine >> i) & 1u) dx[id[i]] = from_f32<T>(listed_grad(a, s_list, terms, g, lane + 32 * i, twice));
+        }
+        if (rank == 0) {
+            const double loss = row_loss(a, s_list, terms, st, lane);
+            if (lane == 0) a.row_loss[row] = (float)loss;
+        }
+        return;
+    }
+    if (!dx) return;
+    auto grad = [&](float x) { return terms.rest * ex2(max_nan((x - st.m) * a.c, kFar)); };
+    auto word = [&](const uint4 &v, int w) {
+        float f[VE];
+        unpack_vec<T>(v, f);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) f[i] = grad(f[i]);
+        put(w, f, listed(w));
+    };
+    int w = w0;
+    for (; w + (U - 1) * TH < end; w += TH * U) {
+        uint4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = r.load_last(w + u * TH);
+#pragma unroll
+        for (int u = 0; u < U; ++u) word(v[u], w + u * TH);
+    }
+    for (; w < end; w += TH) word(r.load_last(w), w);
+    if (edge >= 0) {
+        bool out = false;
+        for (int j = 0; j < a.k; ++j) out |= s_list.id[j] == edge;
+        if (!out) dx[edge] = from_f32<T>(grad(at_edge));
+    }
 }
 
 // A warp per row of at most 32 * E values; lane l holds those at l, l + 32, ..., bit i of `out` says that the i-th is listed.  Returns the
@@ -457,7 +509,7 @@ extern "C" lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, co
                     LPDT_CUDA(cudaFuncSetAttribute(distill_row_kernel<T, TH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDtSmem));
                     attr.mark(dev);
                 }
-                launch_k_cluster(distill_row_kernel<T, TH>, (unsigned)(rows * cs), TH, smem, st, cs, a);
+                launch_k_cluster(distill_row_kernel<T, TH>, (unsigned)(rows * cs), TH + 32, smem, st, cs, a);
                 return LPDT_OK;
             };
             const lpdt_status s = bytes <= 16384 ? go(std::integral_constant<int, 128>()) : bytes <= 65536 ? go(std::integral_constant<int, 256>())
