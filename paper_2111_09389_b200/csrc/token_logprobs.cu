@@ -54,10 +54,11 @@ template <int TH> struct TopList {
     static constexpr int CAP = TH < 256 ? 8 * TH : 2048;
     __align__(16) unsigned long long key[CAP + 8];
     unsigned long long best[kTopMax];
-    static constexpr int ITEMS = 4 * TH;
-    int item[ITEMS];                             // words to look through: twice the first, 1 more for a word by itself and not a turn
-    int again[TH];                               // threads whose every word has to be
-    int count, items, agains;
+    static constexpr int WORDS = 2 * TH;
+    uint4 word[WORDS];                           // words that reach the floor, and the indices of their first elements
+    int index[WORDS];
+    int again[TH];                               // threads whose every word has to be looked at
+    int count, words, agains;
 };
 // (The code behind a row's end runs once a row: a row by itself waits for each of its instructions to be fetched, so it is written to be
 // short, in loops that are not unrolled.  Unrolled over a thread's words and keys the top 20 of one row took 10 us more than none, this 5.)
@@ -110,56 +111,77 @@ struct Best {
         w1 = first ? at : w1;
     }
 };
+// A warp's keys that reach the floor (0: none) onto the list.
+template <int TH>
+__device__ __forceinline__ void push(TopList<TH> &l, unsigned long long key, unsigned long long floor_key, int lane) {
+    const uint32_t who = __ballot_sync(0xffffffffu, key && key >= floor_key);
+    if (!who) return;
+    int to = 0;
+    if (lane == 0) to = atomicAdd(&l.count, __popc(who));
+    to = __shfl_sync(0xffffffffu, to, 0) + __popc(who & ((1u << lane) - 1));
+    if (((who >> lane) & 1u) && to < TopList<TH>::CAP) l.key[to] = key;
+}
 // Puts everything that reaches the floor on the list (`edges`: the row's edges too); its new length, which may exceed the room.  What reaches
-// the floor lies in the turns that reach it; a thread whose second best turn does may have more, so all of its words are looked at.
-// A warp looks through an item, an element a lane.
+// the floor lies in the turns that reach it, whose words that do are kept first, so that memory is waited for once; a thread whose second
+// best turn does may have more, so a warp looks at all of its words.  Then the words are looked through, an element a lane.
 template <typename T, int TH>
 __device__ __noinline__ int collect(const Row<T> r, int begin, int end, bool edges, const Best b, unsigned long long floor_key, TopList<TH> &l) {
     constexpr int VE = Row<T>::VE;
     const float floor_v = floor_key ? key_value(floor_key) : -INFINITY;
     const uint32_t floor_i = (uint32_t)key_index(floor_key);          // the last position that counts among equal ones
     const int tid = threadIdx.x, lane = tid & 31;
-    if (tid == 0) l.count = l.items = l.agains = 0;
+    if (tid == 0) l.count = l.words = l.agains = 0;
     __syncthreads();
     auto in = [&](float v, int w) { return v > floor_v || (v == floor_v && (uint32_t)r.index(w) <= floor_i); };
+    auto keep = [&](const uint4 &v, int w) {
+        if (!in(vec_max<T>(v), w)) return;
+        const int to = atomicAdd(&l.words, 1);
+        if (to < l.WORDS) { l.word[to] = v; l.index[to] = r.index(w); }
+    };
     if (in(b.v1, b.w1)) {
         if (in(b.v2, b.w2)) l.again[atomicAdd(&l.agains, 1)] = begin + tid;
-        else l.item[atomicAdd(&l.items, 1)] = 2 * b.w1 + (b.w1 + (kLpUnroll - 1) * TH < end ? 0 : 1);
+        else {
+            const int words = b.w1 + (kLpUnroll - 1) * TH < end ? kLpUnroll : 1;
+            uint4 v[kLpUnroll];
+#pragma unroll
+            for (int u = 0; u < kLpUnroll; ++u) v[u] = r.load(b.w1 + (u < words ? u : 0) * TH);
+#pragma unroll
+            for (int u = 0; u < kLpUnroll; ++u)
+                if (u < words) keep(v[u], b.w1 + u * TH);
+        }
     }
     __syncthreads();
-    if (l.agains) {                              // a warp for each, a word a lane
+    if (l.agains) {                              // a warp for each, two words a lane at a time
 #pragma unroll 1
         for (int i = tid >> 5; i < l.agains; i += TH / 32)
 #pragma unroll 1
-            for (int w = l.again[i] + lane * TH; w < end; w += 32 * TH)
-                if (in(vec_max<T>(r.load(w)), w)) {
-                    const int to = atomicAdd(&l.items, 1);
-                    if (to < l.ITEMS) l.item[to] = 2 * w + 1;
-                }
+            for (int w = l.again[i] + lane * TH; w < end; w += 64 * TH) {
+                const uint4 v = r.load(w), v2 = r.load(w + 32 * TH < end ? w + 32 * TH : w);
+                keep(v, w);
+                if (w + 32 * TH < end) keep(v2, w + 32 * TH);
+            }
         __syncthreads();
     }
-    const int given = l.items, all = given < l.ITEMS ? given : l.ITEMS, items = all + (edges ? 1 : 0);
+    const int given = l.words, words = given < l.WORDS ? given : l.WORDS, elements = words * VE;
 #pragma unroll 1
-    for (int i = tid >> 5; i < items; i += TH / 32) {
-        const bool edge = i == all;
-        static_assert(kLpUnroll * VE <= 32 && Row<T>::EDGES <= 32, "an item's elements are a warp's lanes");
-        const int what = edge ? 0 : l.item[i];
-        int index = lane < ((what & 1) ? VE : kLpUnroll * VE) ? r.index((what >> 1) + lane / VE * TH) + lane % VE : -1;
-        if (edge) index = lane < Row<T>::EDGES ? r.edge(lane) : -1;
-        unsigned long long key = 0;
-        if (index >= 0) {
-            const float x = to_f32(r.at(index));
-            if (x >= floor_v) key = top_key(x, index);
+    for (int e0 = tid & ~31; e0 < elements; e0 += TH) {
+        const int e = e0 + lane;
+        int index = -1;
+        float x = -INFINITY;
+        if (e < elements) {
+            index = l.index[e / VE] + e % VE;
+            x = to_f32(reinterpret_cast<const T *>(l.word)[e]);
         }
-        const uint32_t who = __ballot_sync(0xffffffffu, key && key >= floor_key);
-        if (!who) continue;
-        int to = 0;
-        if (lane == 0) to = atomicAdd(&l.count, __popc(who));
-        to = __shfl_sync(0xffffffffu, to, 0) + __popc(who & ((1u << lane) - 1));
-        if (((who >> lane) & 1u) && to < TopList<TH>::CAP) l.key[to] = key;
+        unsigned long long key = index >= 0 && x >= floor_v ? top_key(x, index) : 0;
+        push(l, key, floor_key, lane);
+    }
+    if (edges && tid < 32) {
+        const int index = tid < Row<T>::EDGES ? r.edge(tid) : -1;
+        const float x = index >= 0 ? to_f32(r.at(index)) : 0.f;
+        push(l, index >= 0 && x >= floor_v ? top_key(x, index) : 0ull, floor_key, lane);
     }
     __syncthreads();
-    const int n = l.count, least = given > l.ITEMS ? TopList<TH>::CAP + 1 : 0;
+    const int n = l.count, least = given > l.WORDS ? TopList<TH>::CAP + 1 : 0;
     __syncthreads();
     return n > least ? n : least;
 }
@@ -499,7 +521,11 @@ extern "C" lpdt_status lpdt_token_logprobs(int64_t rows, int32_t V, const void *
     const cudaStream_t st = as_stream(stream);
     return with_dtype(dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
-        if (V <= 1024) {
+        // A warp's top k takes a turn for each.  Few rows wait for that: a CTA's, where its warps have lanes enough for a floor, is sooner from
+        // 13 on (one row of 1000 fp32, top 20 6.7 us by a warp, 5.2 by a CTA; top 5 3.7 and 4.9; 8192 rows, top 20 31 and 41).
+        const int full_warps = (int)((int64_t)V * (int64_t)sizeof(T) / 16 / 32);
+        const bool by_cta = V > 1024 || (top_k > 12 && rows <= 4 * kNumSMs && top_k <= 32 * (full_warps < 4 ? full_warps : 4));
+        if (!by_cta) {
             const unsigned grid = (unsigned)ceil_div(rows, 4);
             if (V <= 64) launch_k(logprobs_warp_kernel<T, 2>, grid, 128, 0, st, a);
             else if (V <= 256) launch_k(logprobs_warp_kernel<T, 8>, grid, 128, 0, st, a);
