@@ -230,6 +230,15 @@ __global__ void __launch_bounds__(TH + 32, TH == 512 ? 2 : TH == 256 ? 4 : 8) di
             again |= here && seen;
             if (here && !seen) mine |= 1u << i;
         }
+        if (__any_sync(0xffffffffu, again)) {         // which entry stands for its token does not go by who came first
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int at = id[i] < 0 ? -1 : id[i] - r.index(begin);
+                bool stands = id[i] >= 0 && ((at >= 0 && at < (end - begin) * VE) || (rank == 0 && (id[i] < r.head || id[i] >= r.index(r.words))));
+                for (int j = 0; j < lane + 32 * i && stands; ++j) stands = s_list.id[j] != id[i];
+                mine = (mine & ~(1u << i)) | ((uint32_t)stands << i);
+            }
+        }
     }
     const bool twice = __syncthreads_or(again);
     const uint8_t *bytes = reinterpret_cast<const uint8_t *>(s_bits);
@@ -471,6 +480,7 @@ extern "C" lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, co
     const int64_t rows = (int64_t)nodes * B;
     LPDT_CHECK_ARG(logits && teacher_logprob && teacher_index && loss && row_loss);
     LPDT_CHECK_ARG(aligned(logits, dtype_size(dtype)) && (!dlogits || aligned(dlogits, dtype_size(dtype))));
+    LPDT_CHECK_ARG(aligned(teacher_logprob, 4) && aligned(teacher_index, 4) && aligned(loss, 4) && aligned(row_loss, 4) && aligned(row_weight, 4) && aligned(dev_status, 4));
     LPDT_CHECK_ARG(rows == 1 || (row_stride >= V && (!dlogits || dlogits_row_stride >= V)));
     LPDT_CHECK_ARG(dlogits != logits || rows == 1 || dlogits_row_stride == row_stride);
     if (k > kListMax || V > (1 << 20) || rows > (1 << 27)) return LPDT_ERR_UNSUPPORTED;

@@ -492,7 +492,7 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     if (nodes == 0 || M == 0 || N == 0) return LPDT_OK;
     LPDT_CHECK_ARG(A && sA && B && sB && C);
     LPDT_CHECK_ARG(aligned(A, 16) && aligned(B, 16) && aligned(sA, 4) && aligned(sB, 4));
-    LPDT_CHECK_ARG(aligned(C, dtype_size(c_dtype)) && (!addend || aligned(addend, dtype_size(c_dtype))));
+    LPDT_CHECK_ARG(aligned(C, dtype_size(c_dtype)) && (!addend || aligned(addend, dtype_size(c_dtype))) && aligned(dev_status, 4));
     LPDT_CHECK_ARG((M == 1 || c_row_stride >= N) && (nodes == 1 || c_node_stride >= (M - 1) * c_row_stride + N));
     LPDT_CHECK_ARG(!bias || (aligned(bias, 4) && (nodes == 1 || bias_node_stride >= 0)));
     const int64_t limit = (int64_t)1 << 30;

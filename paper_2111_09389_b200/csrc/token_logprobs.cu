@@ -512,6 +512,7 @@ extern "C" lpdt_status lpdt_token_logprobs(int64_t rows, int32_t V, const void *
     LPDT_CHECK_ARG(logits && aligned(logits, dtype_size(dtype)) && (rows == 1 || row_stride >= V));
     LPDT_CHECK_ARG((logprob || entropy || lse || top_k > 0) && (!logprob || tokens));
     LPDT_CHECK_ARG(top_k == 0 || (top_logprob && top_index));
+    LPDT_CHECK_ARG(aligned(tokens, 4) && aligned(logprob, 4) && aligned(entropy, 4) && aligned(lse, 4) && aligned(top_logprob, 4) && aligned(top_index, 4) && aligned(dev_status, 4));
     if (top_k > kTopMax || V > (1 << 30) || rows > (1 << 27)) return LPDT_ERR_UNSUPPORTED;
     LogprobArgs a = {};
     a.x = logits; a.x_row = rows == 1 ? 0 : row_stride; a.rows = rows; a.V = V;
@@ -552,6 +553,7 @@ extern "C" lpdt_status lpdt_token_logprobs_bwd(int64_t rows, int32_t V, const vo
     if (rows == 0) return LPDT_OK;
     LPDT_CHECK_ARG(logits && dlogits && aligned(logits, dtype_size(dtype)) && aligned(dlogits, dtype_size(dtype)));
     LPDT_CHECK_ARG(rows == 1 || (row_stride >= V && dlogits_row_stride >= V));
+    LPDT_CHECK_ARG(aligned(tokens, 4) && aligned(lse, 4) && aligned(entropy, 4) && aligned(d_logprob, 4) && aligned(d_entropy, 4) && aligned(d_lse, 4));
     LPDT_CHECK_ARG(lse && (!d_logprob || tokens) && (!d_entropy || entropy) && (d_logprob || d_entropy || d_lse));
     // in place: a row's gradient lies where its logits lay, or the two arrays are apart
     LPDT_CHECK_ARG(dlogits != logits || rows == 1 || dlogits_row_stride == row_stride);

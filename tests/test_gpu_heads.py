@@ -161,6 +161,57 @@ def test_rows_that_start_anywhere(V, stride, offset, dtype):
         within(d, ref[2][0], 4 * SUM(V) / rows + torch.finfo(dtype).eps / 2 * np.abs(ref[2][0]) + 2.0 ** -25)
 
 
+def test_offsets_beyond_32_bits():
+    """Rows 2^31 + 8 elements apart: logits, gradients, the quantizer's input and the product's result."""
+    rows, V, k, stride = 3, 5001, 4, 2 ** 31 + 8
+    far = torch.empty((rows - 1) * stride + 8192, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(far, (rows, V), (stride, 1), 0)
+    near = logits_of(rows, V, torch.bfloat16, 8)
+    x.copy_(near)
+    tokens = np.arange(rows)
+    o, _ = check_report(x, tokens, k, 1.0, row_stride=stride)
+    q, s = (torch.empty(rows, api.lpdt_e4m3_pitch(V), dtype=torch.uint8, device="cuda"), torch.empty(rows, api.lpdt_e4m3_scale_pitch(V), dtype=torch.uint8, device="cuda"))
+    qt, st = (torch.empty(V, 16, dtype=torch.uint8, device="cuda"), torch.empty(V, 4, dtype=torch.uint8, device="cuda"))
+    api.lpdt_quantize_e4m3(x, 1, rows, V, q, s, qt, st, x_row_stride=stride)
+    qr, sr = heads.quantize_e4m3(near.double().numpy())
+    assert np.array_equal(q.cpu().numpy()[:, :V], qr) and np.array_equal(s.cpu().numpy()[:, :sr.shape[1]], sr)
+    assert np.array_equal(qt.cpu().numpy()[:, :rows], heads.quantize_e4m3(near.double().numpy().T)[0])
+    loss, row_loss = torch.empty(1, device="cuda"), torch.empty(rows, device="cuda")
+    lists = o["top_logprob"], o["top_index"]
+    api.lpdt_distill_topk(1, rows, V, x, k, *lists, loss, row_loss, dlogits=x, row_stride=stride, dlogits_row_stride=stride)
+    ref = heads.distill_topk(near.double().numpy()[None], lists[0].cpu().numpy()[None], lists[1].cpu().numpy()[None], True)
+    within(x, ref[2][0], 4 * SUM(V) / rows + 2.0 ** -8 * np.abs(ref[2][0]) + 2.0 ** -25)
+    x.copy_(near)
+    api.lpdt_token_logprobs_bwd(rows, V, x, torch.arange(rows, dtype=torch.int32, device="cuda"), o["lse"], o["entropy"], x,
+                                d_logprob=torch.ones(rows, device="cuda"), row_stride=stride, dlogits_row_stride=stride)
+    want = heads.token_logprobs_bwd(near.double().numpy(), tokens, np.ones(rows))
+    within(x, want, 64 * U + 2.0 ** -8 * np.abs(want) + 2.0 ** -25)
+    api.lpdt_matmul_e4m3(1, rows, V, 16, qt.view(-1, 16), st, qt, st, x, c_row_stride=stride)         # its first three rows with all
+    v = heads.dequantize_e4m3(qt.cpu().numpy(), st.cpu().numpy()[:, :1])
+    v[:, rows:] = 0
+    within(x, v[:rows] @ v.T, 2.0 ** -8 * np.abs(v[:rows] @ v.T) + 1e-5)
+
+
+def test_the_same_bits_every_time():
+    """Lists with tokens listed twice, ties among the top: ten calls on two streams at once give the same bits."""
+    rows, V, k = 6, 70001, 64
+    x = logits_of(rows, V, torch.bfloat16, 1).cuda()
+    value, index = lists_of(1, rows, V, k, 3, duplicates=True)
+    index[..., k // 2:] = index[..., :k // 2]
+    value, index = torch.from_numpy(value).cuda(), torch.from_numpy(index).cuda()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for i in range(10):
+        with torch.cuda.stream(streams[i % 2]):
+            loss, row_loss, d = torch.empty(1, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+            api.lpdt_distill_topk(1, rows, V, x, k, value, index, loss, row_loss, dlogits=d)
+            o, _ = report(x, np.zeros(rows), k)
+            got.append([loss, row_loss, d] + [o[n] for n in sorted(o)])
+    torch.cuda.synchronize()
+    for g in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(g, got[0]))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows,V,temperature", [(1, 1, 1.0), (40, 10, 2.0), (3, 333, 0.7), (2, 1025, 1.0), (5, 32003, 1.0), (1, 140000, 0.5)])
 @pytest.mark.parametrize("which", ["logprob", "entropy", "lse", "all"])

@@ -74,7 +74,7 @@ def test_product_refusals():
         assert call(**empty) == OK
     for bad in (dict(nodes=-1), dict(M=-1), dict(N=-1), dict(K=0), dict(K=-5), dict(A=0), dict(sA=0), dict(B=0), dict(sB=0), dict(C=0),
                 dict(c_dtype=7), dict(A=P + 8), dict(B=P + 4), dict(sA=P + 2), dict(sB=P + 1), dict(C=P + 2), dict(addend=P + 1),
-                dict(c_row=4), dict(c_node=14), dict(bias=P, bias_node=-1), dict(bias=P + 2)):
+                dict(c_row=4), dict(c_node=14), dict(bias=P, bias_node=-1), dict(bias=P + 2), dict(status=P + 1)):
         assert call(**bad) == INVALID, bad
     assert call(K=(1 << 30) + 1) == UNSUPPORTED and call(M=1 << 31, c_node=1 << 40) == UNSUPPORTED
 
@@ -135,7 +135,8 @@ def test_report_refusals():
     assert call(rows=0) == OK and call(rows=0, x=0) == OK
     for bad in (dict(rows=-1), dict(V=0), dict(V=-3), dict(x=0), dict(dtype=9), dict(stride=8), dict(temperature=0.0), dict(temperature=-1.0),
                 dict(temperature=float("nan")), dict(temperature=float("inf")), dict(tokens=0), dict(k=10), dict(k=-1), dict(top=0),
-                dict(index=0), dict(logprob=0, entropy=0, lse=0, k=0), dict(x=P + 2), dict(x=P + 1, dtype=2)):
+                dict(index=0), dict(logprob=0, entropy=0, lse=0, k=0), dict(x=P + 2), dict(x=P + 1, dtype=2), dict(tokens=P + 2), dict(lse=P + 1),
+                dict(top=P + 3), dict(status=P + 2)):
         assert call(**bad) == INVALID, bad
     assert call(k=129, V=200, stride=200) == UNSUPPORTED and call(V=(1 << 30) + 1, stride=1 << 31) == UNSUPPORTED and call(rows=1 << 28) == UNSUPPORTED
 
@@ -146,7 +147,7 @@ def test_report_gradient_refusals():
     call = lambda **kw: _lib.lib().lpdt_token_logprobs_bwd(*[{**base, **kw}[n] for n in names])
     assert call(rows=0) == OK
     for bad in (dict(rows=-1), dict(V=0), dict(x=0), dict(dx=0), dict(lse=0), dict(tokens=0), dict(entropy=0), dict(g=0, h=0, l=0), dict(dstride=8),
-                dict(stride=1), dict(dx=P, dstride=10), dict(dx=P + 1), dict(temperature=0.0), dict(dtype=3)):
+                dict(stride=1), dict(dx=P, dstride=10), dict(dx=P + 1), dict(temperature=0.0), dict(dtype=3), dict(lse=P + 2), dict(h=P + 1)):
         assert call(**bad) == INVALID, bad
     assert call(rows=1 << 28) == UNSUPPORTED
 
@@ -159,6 +160,26 @@ def test_distillation_refusals():
     assert call(nodes=0) == OK
     for bad in (dict(nodes=-1), dict(B=0), dict(V=0), dict(x=0), dict(value=0), dict(index=0), dict(loss=0), dict(row_loss=0), dict(k=0), dict(k=-2),
                 dict(tail=2), dict(stride=8), dict(dstride=3), dict(dx=P, dstride=12), dict(temperature=0.0), dict(temperature=float("nan")),
-                dict(dtype=-1), dict(x=P + 1), dict(dx=2 * P + 2)):
+                dict(dtype=-1), dict(x=P + 1), dict(dx=2 * P + 2), dict(value=P + 2), dict(index=P + 1), dict(weight=P + 3), dict(loss=P + 2)):
         assert call(**bad) == INVALID, bad
     assert call(k=129) == UNSUPPORTED and call(V=(1 << 20) + 1, stride=1 << 21, dstride=1 << 21) == UNSUPPORTED
+
+
+def test_recorded_sequences_take_the_calls():
+    """Empty calls of each run in a recorded sequence; a bad one is refused there as by itself."""
+    import ctypes as C
+    from paper_2111_09389_b200 import api
+    f = C.c_uint32.from_buffer(C.c_float(1.0)).value
+    items = {"lpdt_quantize_e4m3": [0, 0, 0, 1, 1, 1, 1, 0, 0, 0, 0], "lpdt_matmul_e4m3": [0, 1, 1, 1] + [0] * 12,
+             "lpdt_token_logprobs": [0, 5, 0, 0, 5, f] + [0] * 8, "lpdt_token_logprobs_bwd": [0, 5, 0, 0, 5, f] + [0] * 8,
+             "lpdt_distill_topk": [0, 1, 5, 0, 0, 5, f, 1, 0, 0, 1] + [0] * 6}
+    words = []
+    for name, args in items.items():
+        i = api.lpdt_call_id(name)
+        assert i >= 0, name
+        words += [i, 0] + args
+    code = lambda w: (C.c_uint64 * len(w))(*w)
+    assert api.lpdt_run_calls(code(words), [0]) == (0, 4)
+    words[-8] = 7                                              # tail
+    words[-17] = 1                                             # nodes
+    assert api.lpdt_run_calls(code(words), [0])[0] == INVALID
