@@ -69,8 +69,8 @@ __device__ __forceinline__ void scaled(uint32_t w, float s0, float s1, float *f,
     f[1] = v.y * s1;
 }
 __device__ __forceinline__ void scaled(uint32_t w, float s0, float s1, float *f, __nv_bfloat16) {
-    f[0] = __uint_as_float(w << 16) * s0;
-    f[1] = __uint_as_float(w & 0xffff0000u) * s1;
+    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&w), __floats2bfloat162_rn(s0, s1));
+    unpack_word(*reinterpret_cast<const uint32_t *>(&p), f, __nv_bfloat16());
 }
 
 struct E4m3Args {
