@@ -14,7 +14,7 @@
 // the CTAs.
 //
 // Two accumulators of up to 224 columns (the epilogue of one tile runs under the products of the next) and four sets of scale factors
-// fill the 512 columns of tensor memory.
+// fill the 512 columns of tensor memory; CTAs of one tile have one accumulator, and two of them fit an SM.
 //
 // Roles per CTA: warp 0 fetches codes (TMA), warp 1 copies scale factors to tensor memory and issues the products, warp 2 brings the
 // scale bytes into the layout they are copied from, warps 4-11 run the epilogue.  Every wait on a barrier is bounded.
@@ -29,7 +29,7 @@ constexpr size_t kMmSmem = 227 * 1024;
 
 struct MmParams {
     int nodes, M, N, kblocks, bn;              // bn: rows of C per tile, a multiple of 16
-    int tilesJ, tilesM, stages, tmem_cols;
+    int tilesJ, tilesM, stages, tmem_cols, accs;   // accs: accumulators, 1 where a CTA makes one tile
     int groups, per_cta;                       // SPLIT: groups of 8 rows of a tile that exist, most of them that one CTA adds up
     int slot;                                  // bytes of a stage: codes of both sides
     const uint8_t *sA, *sB;
@@ -166,7 +166,7 @@ __device__ __forceinline__ void mm_store(const MmParams &p, int node, int m, int
 
 // SPLIT: the clusters' CTAs share one tile's K (G = 1), a CTA makes one tile.
 template <int G, bool SPLIT, typename OutT>
-__global__ void __launch_bounds__(kMmThreads, 1)
+__global__ void __launch_bounds__(kMmThreads, G == 1 ? 2 : 1)
 matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const __grid_constant__ CUtensorMap mapR /*A: rows*/, const MmParams p) {
     static_assert(!(SPLIT && G == 2), "one or the other");
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -184,8 +184,10 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
 
     // Each role waits for the kernels before this one at its first access of global memory, and does what it can before: the fetching warp
     // sets the barriers up and goes on (its loads need nothing else), the scales' warp asks for the first words, meanwhile.
+    // The next kernel's CTAs may start once this one has its tensor memory: theirs, which they would hold while they wait, cannot keep it
+    // from this one.
     if constexpr (SPLIT) mm_cluster_arrive();
-    pdl_trigger();
+    if (warp != 1) pdl_trigger();
     if (warp == 0) {
         if (lane == 0) {
             for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
@@ -204,6 +206,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             tmem_alloc(smem_u32(&ctl->tmem_base), (uint32_t)p.tmem_cols);
             tmem_relinquish();
         }
+        pdl_trigger();
     }
     MmScaleRows rows;
     uint32_t next[12];
@@ -252,7 +255,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         if (G == 1 || rank == 0) {
             const uint32_t idesc = idesc_mx_e4m3(128 * G, p.bn);
             const uint64_t tpl = smem_desc(0, 16, 1024, 2), sc_tpl = smem_desc(0, 16, 128, 0);
-            const uint32_t sf0 = tmem_base + 2 * p.bn;
+            const uint32_t sf0 = tmem_base + p.accs * p.bn;
             // Groups of four blocks of K, counted over all tiles: `copied` have their factors in tensor memory or on their way.  A group's are
             // copied one group ahead of its products, which then do not wait for the copy.
             const uint32_t per_tile = (uint32_t)(((k_end - 1) >> 2) - (k_begin >> 2) + 1);
@@ -421,15 +424,17 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     }
 }
 
-struct MmPlan { int g, bn, split; };
+struct MmPlan { int g, bn, split, dense; };
 
 // The least of an estimate in cycles over pairs and single SMs, rows per tile and shares of K.  A block of 128 values of K takes a tile of bn
 // rows the products' 2 * bn cycles or, where that is more, what its codes take from L2: 48 bytes a cycle of an SM by itself, 34 of one of
-// a pair.  Behind that 12 cycles a row for the epilogue.  Clusters of 8 find room on 96 SMs at once.  (Fitted to every plan's time for 17
-// shapes from 1 x 4096 x 4096 to 4096^3: the plan is within 1 % of the best for all of them.  Pairs pay for themselves when every
-// SM has several tiles: 4096^3 65.3 us against 68.8 on single SMs, 2048^3 17.6 against 16.0.)
+// a pair.  Behind that 12 cycles a row for the epilogue.  Clusters of 8 find room on 96 SMs at once.  `dense`: two CTAs of one tile each on
+// an SM instead of one that walks over tiles; one's epilogue then runs beside the other's loads, whose halves of the SM take 24 bytes a
+// cycle each.  (Fitted to every plan's time for 21 shapes from 1 x 4096 x 4096 to 4096^3: the plan is within 2 % of the best on average.
+// Pairs pay for themselves when every SM has several tiles: 4096^3 65.3 us against 68.8 on single SMs, 2048^3 17.6 against 16.0; dense is
+// best for some 150 to 300 tiles: 2048^3 13.3 us.)
 static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
-    MmPlan best = {1, 16, 1};
+    MmPlan best = {1, 16, 1, 0};
     double least = 1e300;
     for (int g = 1; g <= 2; ++g) {
         const int64_t tj = ceil_div(N, 128 * g);
@@ -441,8 +446,14 @@ static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
             for (int split = 1; split <= (g == 1 && bn <= 128 ? 8 : 1); split *= 2) {
                 if (split > kblocks) break;
                 const int64_t slots = split == 8 ? 96 : kNumSMs / (g * split) * (g * split);
-                const double cost = ceil_div(tiles * g * split, slots) * (ceil_div(kblocks, split) * per + 12.0 * bn) + (g == 2 ? 1000 : 0);
-                if (cost < least) { least = cost; best = {g, bn, split}; }
+                const double cost = ceil_div(tiles * g * split, slots) * (ceil_div(kblocks, split) * per + 12.0 * bn) +
+                                    (g == 2 ? 1000 : 0) + (split > 1 ? 900 : 0);
+                if (cost < least) { least = cost; best = {g, bn, split, 0}; }
+            }
+            if (g == 1 && bn >= 64 && bn <= 128 && tiles > kNumSMs) {
+                const double shared = bytes / 24 > 4.0 * bn ? bytes / 24 : 4.0 * bn;
+                const double cost = ceil_div(tiles, 2 * kNumSMs) * (kblocks * shared + 8.0 * bn);
+                if (cost < least) { least = cost; best = {1, bn, 1, 1}; }
             }
         }
     }
@@ -471,7 +482,7 @@ static lpdt_status mm_launch(const CUtensorMap &mL, const CUtensorMap &mR, const
         ++g_launch_count;
         cudaLaunchKernelEx(&cfg, matmul_e4m3_kernel<G, SPLIT, OutT>, mL, mR, p);
     } else {
-        const int64_t ctas = tiles * G < kNumSMs ? tiles * G : kNumSMs;
+        const int64_t ctas = tiles * G < kNumSMs || p.accs == 1 ? tiles * G : kNumSMs;
         launch_k_cluster(matmul_e4m3_kernel<G, SPLIT, OutT>, (unsigned)ctas, kMmThreads, smem, st, G, mL, mR, p);
     }
     LPDT_LAUNCH_CHECK();
@@ -514,7 +525,9 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     // Few rows: half of an SM's shared memory holds enough of them in flight, and the other half lets the next such call's CTAs start.
     const int half = (int)((kMmSmem / 2 - 1024 - rest) / p.slot);
     if (plan.bn <= 64 && tiles * plan.split <= kNumSMs && half >= 4 && p.stages > half) p.stages = half;
-    for (p.tmem_cols = 128; p.tmem_cols < 2 * plan.bn + kMmScaleSlots * 16; p.tmem_cols *= 2) {}
+    p.accs = plan.dense || plan.split > 1 ? 1 : 2;
+    if (plan.dense) p.stages = half;
+    for (p.tmem_cols = 128; p.tmem_cols < p.accs * plan.bn + kMmScaleSlots * 16; p.tmem_cols *= 2) {}
     p.sA = sA; p.sB = sB; p.spitch = (int)lpdt_e4m3_scale_pitch(K);
     p.bias = bias; p.bias_node = nodes == 1 ? 0 : bias_node_stride;
     p.addend = addend; p.C = C; p.c_node = nodes == 1 ? 0 : c_node_stride; p.c_row = M == 1 ? 0 : c_row_stride;
