@@ -428,11 +428,12 @@ struct MmPlan { int g, bn, split, dense; };
 
 // The least of an estimate in cycles over pairs and single SMs, rows per tile and shares of K.  A block of 128 values of K takes a tile of bn
 // rows the products' 2 * bn cycles or, where that is more, what its codes take from L2: 48 bytes a cycle of an SM by itself, 34 of one of
-// a pair.  Behind that 12 cycles a row for the epilogue.  Clusters of 8 find room on 96 SMs at once.  `dense`: two CTAs of one tile each on
-// an SM instead of one that walks over tiles; one's epilogue then runs beside the other's loads, whose halves of the SM take 24 bytes a
-// cycle each.  (Fitted to every plan's time for 21 shapes from 1 x 4096 x 4096 to 4096^3: the plan is within 2 % of the best on average.
-// Pairs pay for themselves when every SM has several tiles: 4096^3 65.3 us against 68.8 on single SMs, 2048^3 17.6 against 16.0; dense is
-// best for some 150 to 300 tiles: 2048^3 13.3 us.)
+// a pair.  An epilogue of some 8 cycles a row runs under the next tile's products, the last one by itself.  Clusters of 8 find room on 96
+// SMs at once.  `dense`: two CTAs of one tile each on an SM instead of one that walks over tiles, where one round of them is enough; one's
+// epilogue then runs beside the other's loads, whose halves of the SM take 24 bytes a cycle each.  (Fitted to every plan's time for 29
+// shapes from 1 x 4096 x 4096 to 4096^3: the plan is within 2 % of the best on average.  Pairs pay for themselves when every SM has
+// several tiles of long K: 4096^3 65.0 us against 67.7 on single SMs, 2048^3 17.6 against 16.0; dense 2048^3 13.3 us; narrow tiles or
+// dense ones would cost many tiles of short K a third: 2 x 4188 x 4744 x 259 42.9 us, 55.4 by a plan without the epilogue's share.)
 static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
     MmPlan best = {1, 16, 1, 0};
     double least = 1e300;
@@ -446,13 +447,14 @@ static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
             for (int split = 1; split <= (g == 1 && bn <= 128 ? 8 : 1); split *= 2) {
                 if (split > kblocks) break;
                 const int64_t slots = split == 8 ? 96 : kNumSMs / (g * split) * (g * split);
-                const double cost = ceil_div(tiles * g * split, slots) * (ceil_div(kblocks, split) * per + 12.0 * bn) +
-                                    (g == 2 ? 1000 : 0) + (split > 1 ? 900 : 0);
+                const double waves = (double)ceil_div(tiles * g * split, slots), k = ceil_div(kblocks, split) * per;
+                const double cost = split > 1 ? waves * (k + 12.0 * bn) + 900
+                                              : waves * (k + 200 > 8.0 * bn ? k + 200 : 8.0 * bn) + 12.0 * bn + (g == 2 ? 1500 : 0);
                 if (cost < least) { least = cost; best = {g, bn, split, 0}; }
             }
-            if (g == 1 && bn >= 64 && bn <= 128 && tiles > kNumSMs) {
+            if (g == 1 && bn >= 64 && bn <= 128 && tiles > kNumSMs && tiles <= 2 * kNumSMs) {
                 const double shared = bytes / 24 > 4.0 * bn ? bytes / 24 : 4.0 * bn;
-                const double cost = ceil_div(tiles, 2 * kNumSMs) * (kblocks * shared + 8.0 * bn);
+                const double cost = kblocks * shared + 8.0 * bn;
                 if (cost < least) { least = cost; best = {1, bn, 1, 1}; }
             }
         }

@@ -119,7 +119,7 @@ def device_operands(ops, K):
 SHAPES = [(1, 1, 16, 128), (1, 1, 4096, 4096), (1, 1, 1, 1), (2, 3, 5, 7), (1, 17, 300, 1000), (3, 64, 200, 513), (4, 150, 130, 257),
           (1, 128, 128, 129), (1, 33, 1, 8191), (1, 240, 256, 384), (1, 500, 1023, 640), (1, 1025, 2049, 300), (2, 700, 1500, 1200),
           (1, 2048, 2048, 512), (5, 1, 129, 2000), (1, 4100, 515, 130),
-          (1, 90, 4100, 2900), (1, 3000, 5000, 1000), (2, 4188, 4744, 259)]
+          (1, 90, 4100, 2900), (2, 1615, 4810, 3788), (3, 433, 4791, 2776), (2, 4188, 4744, 259)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
