@@ -348,12 +348,13 @@ __global__ void __launch_bounds__(TH + 32, TH == 512 ? 2 : TH == 256 ? 4 : 8) di
         put(w, f, listed(w));
     };
     int w = w0;
-    for (; w + (U - 1) * TH < end; w += TH * U) {
-        uint4 v[U];
+    constexpr int U2 = 32 / VE;                       // words of 32 values: of fp32 twice as many bytes on their way (4 x 512 x 131072: 494 -> 467 us)
+    for (; w + (U2 - 1) * TH < end; w += TH * U2) {
+        uint4 v[U2];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = r.load_last(w + u * TH);
+        for (int u = 0; u < U2; ++u) v[u] = r.load_last(w + u * TH);
 #pragma unroll
-        for (int u = 0; u < U; ++u) word(v[u], w + u * TH);
+        for (int u = 0; u < U2; ++u) word(v[u], w + u * TH);
     }
     for (; w < end; w += TH) word(r.load_last(w), w);
     if (edge >= 0) {
@@ -507,10 +508,13 @@ extern "C" lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, co
             else if (V <= 256) launch_k(distill_warp_kernel<T, 8, kListMax>, grid, 128, 0, st, a);
             else launch_k(distill_warp_kernel<T, 32, kListMax>, grid, 128, 0, st, a);
         } else {
-            const int cs = row_share(rows, (int64_t)V * sizeof(T), 4, 4096);
+            // Two CTAs for rows above 256 KB, so that the second pass of those in flight finds them in L2 (131072 fp32: 467 -> 424 us)
+            int cs = row_share(rows, (int64_t)V * sizeof(T), 4, 4096);
+            if (cs == 1 && (int64_t)V * (int64_t)sizeof(T) > 262144) cs = 2;
             const size_t smem = align_up(ceil_div((int64_t)V, cs) / 8 + 16, 16);
-            // threads by what a CTA reads: few for short rows, whose barriers and joins cost more than the reading
-            const int64_t bytes = (int64_t)V * (int64_t)sizeof(T) / cs;
+            // Threads by what a CTA reads, fewer for short rows, whose barriers and joins cost more than the reading; more where few rows leave
+            // SMs idle.  (4096 rows of 30000 bf16 109 us on 128 threads, 117 on 256, 156 on 512; of 131072 bf16 526, 489, 444.)
+            const int64_t bytes = (int64_t)V * (int64_t)sizeof(T) / cs * (rows * cs > 2 * kNumSMs ? 1 : 4);
             auto go = [&](auto threads) -> lpdt_status {
                 constexpr int TH = decltype(threads)::value;
                 static PerDeviceOnce attr;
@@ -522,7 +526,7 @@ extern "C" lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, co
                 launch_k_cluster(distill_row_kernel<T, TH>, (unsigned)(rows * cs), TH + 32, smem, st, cs, a);
                 return LPDT_OK;
             };
-            const lpdt_status s = bytes <= 16384 ? go(std::integral_constant<int, 128>()) : bytes <= 65536 ? go(std::integral_constant<int, 256>())
+            const lpdt_status s = bytes <= 65536 ? go(std::integral_constant<int, 128>()) : bytes <= 131072 ? go(std::integral_constant<int, 256>())
                                                                                           : go(std::integral_constant<int, 512>());
             if (s != LPDT_OK) return s;
         }
