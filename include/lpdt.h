@@ -678,8 +678,8 @@ lpdt_status lpdt_token_logprobs_bwd(int64_t rows, int32_t V, const void *logits,
  * logits, dlogits (nullable: loss only; may be the logits themselves with the same stride) : rows n*B + b as above.
  * teacher_logprob fp32, teacher_index int32 : [nodes][B][k], k 1 to 128 (it may exceed V).  An index < 0 is no entry; one
  * >= V is none either and puts LPDT_ERR_INVALID_ARG into dev_status.  A token may be listed more than once.
- * row_weight : fp32 [nodes][B] (nullable: 1).  A row of weight 0 is not read: row_loss 0, gradient 0; so is a student's row
- * of nothing but mask values (lse < -1e30).  loss fp32 [nodes], row_loss fp32 [nodes][B].
+ * row_weight : fp32 [nodes][B] (nullable: 1).  A row of weight 0 has row_loss 0 and gradient 0 whatever it holds; so has a
+ * student's row of nothing but mask values (lse < -1e30).  loss fp32 [nodes], row_loss fp32 [nodes][B].
  * Errors: INVALID_ARG, UNSUPPORTED (k > 128, V > 2^20, nodes*B > 2^27), CUDA. */
 lpdt_status lpdt_distill_topk(int32_t nodes, int32_t B, int32_t V, const void *logits, lpdt_dtype dtype, int64_t row_stride,
                               float temperature, int32_t k, const float *teacher_logprob, const int32_t *teacher_index,

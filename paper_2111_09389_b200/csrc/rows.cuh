@@ -93,7 +93,8 @@ template <typename H> __device__ __forceinline__ uint4 same_word(H h) {
 }
 
 // Running sums relative to the maximum so far: s = sum 2^t, w = sum 2^t * t with t = (x - m) * c, c = log2(e) / temperature.
-// A value that is -inf, or far below m, counts as t = -10000: 2^t = 0 and no 0 * inf.  NaN passes through max_nan and stays.
+// A value that is -inf, or far below m, counts as t = -10000 where w is taken: 2^t = 0 and no 0 * inf.  NaN passes through max_nan and
+// stays.  Without w, 2^-inf = 0 is enough (4 x 1024 x 131072 distilled: 443 -> 429 us, with the second pass two values at a time).
 // m starts at the lowest float, so a row of nothing but -inf ends with s = 0, one of lowest floats is uniform.
 constexpr float kFar = -10000.f;
 struct Stats {
@@ -136,8 +137,10 @@ template <int N, bool W> __device__ __forceinline__ void accumulate(Stats &a, co
     for (int i = 0; i < N; i += 2) {
         float t0, t1;
         unpack2(mul2(add2(pack2(f[i], f[i + 1]), minus_m), c2), t0, t1);
-        t0 = max_nan(t0, kFar);
-        t1 = max_nan(t1, kFar);
+        if (W) {
+            t0 = max_nan(t0, kFar);
+            t1 = max_nan(t1, kFar);
+        }
         const F2 e = pack2(ex2(t0), ex2(t1));
         s = add2(s, e);
         if (W) w = fma2(e, pack2(t0, t1), w);
