@@ -188,9 +188,8 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     // Each role waits for the kernels before this one at its first access of global memory, and does what it can before: the fetching warp
     // sets the barriers up and goes on (its loads need nothing else), the scales' warp asks for the first words, meanwhile.
     // The next kernel's CTAs may start once this one has its tensor memory: theirs, which they would hold while they wait, cannot keep it
-    // from this one.
+    // from this one.  A CTA's first trigger, by whichever warp, is the one that counts, so only the warp that allocates gives it.
     if constexpr (SPLIT) mm_cluster_arrive();
-    if (warp != 1) pdl_trigger();
     if (warp == 0) {
         if (lane == 0) {
             for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
