@@ -305,7 +305,8 @@ lpdt_status lpdt_qconv_bwd_weight_affine(const lpdt_conv_desc *d, const uint8_t 
  *            rows the second, so the three products of a linear layer Y = X W^T are lpdt_matmul_e4m3 of
  *            (X, W), (dY, W transposed) and (dY transposed, X transposed).
  * scale and scale_t need no alignment here.  Codes are written up to their pitch (zeros behind the last column).
- * Errors: INVALID_ARG, UNSUPPORTED (a dimension above 2^30, 2^31 blocks or more), CUDA.  Empty matrices are a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED (a dimension above 2^30, 2^31 blocks or more; the transposed form also above 65535 nodes
+ * or 65535 * 128 rows), CUDA.  Empty matrices are a no-op.
  */
 int64_t lpdt_e4m3_pitch(int64_t cols);
 int64_t lpdt_e4m3_scale_pitch(int64_t cols);

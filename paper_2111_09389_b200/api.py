@@ -90,6 +90,24 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _typed(t, dtype):
+    """Address of a tensor that has to be of that type: for calls beside whose own several types another is easily passed."""
+    assert t is None or t.dtype == dtype, f"{dtype} expected, not {t.dtype}"
+    return _ptr(t)
+
+
+def _f32(t):
+    return _typed(t, torch.float32)
+
+
+def _i32(t):
+    return _typed(t, torch.int32)
+
+
+def _u8(t):
+    return _typed(t, torch.uint8)
+
+
 def _stream():
     return torch.cuda.current_stream().cuda_stream
 
@@ -284,8 +302,8 @@ def lpdt_quantize_e4m3(x, nodes, rows, cols, q=None, scale=None, qt=None, scale_
     """x fp32, bf16 or fp16; q, scale: blocks of 128 along the rows; qt, scale_t: of the transpose."""
     xr = cols if x_row_stride is None else x_row_stride
     xn = rows * xr if x_node_stride is None else x_node_stride
-    _check("lpdt_quantize_e4m3", lib().lpdt_quantize_e4m3(_ptr(x), _dtype(x), nodes, rows, cols, xn, xr, _ptr(q), _ptr(scale),
-                                                          _ptr(qt), _ptr(scale_t), _stream_handle()))
+    _check("lpdt_quantize_e4m3", lib().lpdt_quantize_e4m3(_ptr(x), _dtype(x), nodes, rows, cols, xn, xr, _u8(q), _u8(scale),
+                                                          _u8(qt), _u8(scale_t), _stream_handle()))
 
 
 def lpdt_matmul_e4m3(nodes, M, N, K, A, sA, B, sB, C, bias=None, bias_node_stride=0, addend=None, c_row_stride=None,
@@ -295,8 +313,8 @@ def lpdt_matmul_e4m3(nodes, M, N, K, A, sA, B, sB, C, bias=None, bias_node_strid
     cn = M * cr if c_node_stride is None else c_node_stride
     assert addend is None or addend.dtype == C.dtype, "addend has the type of C"
     _check("lpdt_matmul_e4m3", lib().lpdt_matmul_e4m3(
-        nodes, M, N, K, _ptr(A), _ptr(sA), _ptr(B), _ptr(sB), _ptr(bias), bias_node_stride, _ptr(addend), _ptr(C), _dtype(C),
-        cn, cr, _ptr(dev_status), _stream_handle()))
+        nodes, M, N, K, _u8(A), _u8(sA), _u8(B), _u8(sB), _f32(bias), bias_node_stride, _ptr(addend), _ptr(C), _dtype(C),
+        cn, cr, _i32(dev_status), _stream_handle()))
 
 
 def lpdt_range_evonorm_fwd(nodes, B, H, W, Cc, groups, eps, x, v, gamma, beta, param_node_stride, y,
@@ -528,8 +546,8 @@ def lpdt_token_logprobs(rows, V, logits, tokens=None, logprob=None, entropy=None
                         top_k=0, temperature=1.0, row_stride=None, dev_status=None):
     """logits fp32, bf16 or fp16 [rows][V]; tokens, top_index int32; the rest fp32."""
     _check("lpdt_token_logprobs", lib().lpdt_token_logprobs(
-        rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _ptr(tokens), _ptr(logprob),
-        _ptr(entropy), _ptr(lse), top_k, _ptr(top_logprob), _ptr(top_index), _ptr(dev_status), _stream_handle()))
+        rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _i32(tokens), _f32(logprob),
+        _f32(entropy), _f32(lse), top_k, _f32(top_logprob), _i32(top_index), _i32(dev_status), _stream_handle()))
 
 
 def lpdt_token_logprobs_bwd(rows, V, logits, tokens, lse, entropy, dlogits, d_logprob=None, d_entropy=None, d_lse=None,
@@ -537,8 +555,8 @@ def lpdt_token_logprobs_bwd(rows, V, logits, tokens, lse, entropy, dlogits, d_lo
     """lse, entropy as the forward wrote them; dlogits of the logits' type."""
     assert dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
     _check("lpdt_token_logprobs_bwd", lib().lpdt_token_logprobs_bwd(
-        rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _ptr(tokens), _ptr(lse),
-        _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(d_lse), _ptr(dlogits),
+        rows, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, _i32(tokens), _f32(lse),
+        _f32(entropy), _f32(d_logprob), _f32(d_entropy), _f32(d_lse), _ptr(dlogits),
         V if dlogits_row_stride is None else dlogits_row_stride, _stream_handle()))
 
 
@@ -547,9 +565,9 @@ def lpdt_distill_topk(nodes, B, V, logits, k, teacher_logprob, teacher_index, lo
     """teacher_logprob fp32, teacher_index int32 [nodes][B][k]; dlogits of the logits' type."""
     assert dlogits is None or dlogits.dtype == logits.dtype, "dlogits has the type of the logits"
     _check("lpdt_distill_topk", lib().lpdt_distill_topk(
-        nodes, B, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, k, _ptr(teacher_logprob),
-        _ptr(teacher_index), int(tail), _ptr(row_weight), _ptr(loss), _ptr(row_loss), _ptr(dlogits),
-        V if dlogits_row_stride is None else dlogits_row_stride, _ptr(dev_status), _stream_handle()))
+        nodes, B, V, _ptr(logits), _dtype(logits), V if row_stride is None else row_stride, temperature, k, _f32(teacher_logprob),
+        _i32(teacher_index), int(tail), _f32(row_weight), _f32(loss), _f32(row_loss), _ptr(dlogits),
+        V if dlogits_row_stride is None else dlogits_row_stride, _i32(dev_status), _stream_handle()))
 
 
 def lpdt_colsum(nodes, B, Cc, x, out, out_node_stride):

@@ -183,3 +183,19 @@ def test_recorded_sequences_take_the_calls():
     words[-8] = 7                                              # tail
     words[-17] = 1                                             # nodes
     assert api.lpdt_run_calls(code(words), [0])[0] == INVALID
+
+
+def test_the_binding_refuses_other_types():
+    """64-bit token numbers, log probabilities of 16 bits and codes that are no bytes would be read as something else."""
+    import torch
+    from paper_2111_09389_b200 import api
+    z, i64, b16, i8 = torch.zeros(4), torch.zeros(4, dtype=torch.int64), torch.zeros(4, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int8)
+    on_gpu = type("Logits", (), dict(is_cuda=True, dtype=torch.float32, data_ptr=lambda self: P))()
+    for bad, call in ((i64, lambda t: api.lpdt_token_logprobs(1, 4, on_gpu, tokens=t)), (b16, lambda t: api.lpdt_token_logprobs(1, 4, on_gpu, lse=t)),
+                      (i64, lambda t: api.lpdt_token_logprobs_bwd(1, 4, on_gpu, t, None, None, on_gpu)),
+                      (b16, lambda t: api.lpdt_distill_topk(1, 1, 4, on_gpu, 1, t, None, None, None)),
+                      (z, lambda t: api.lpdt_distill_topk(1, 1, 4, on_gpu, 1, None, t, None, None)),
+                      (i8, lambda t: api.lpdt_quantize_e4m3(on_gpu, 1, 1, 4, q=t)), (z, lambda t: api.lpdt_matmul_e4m3(1, 1, 1, 1, t, None, None, None, on_gpu)),
+                      (b16, lambda t: api.lpdt_matmul_e4m3(1, 1, 1, 1, None, None, None, None, on_gpu, bias=t))):
+        with pytest.raises(AssertionError, match="expected, not " + str(bad.dtype)):
+            call(bad)
