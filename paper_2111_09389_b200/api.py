@@ -90,22 +90,18 @@ def _ptr(t):
     return t.data_ptr()
 
 
-def _typed(t, dtype):
-    """Address of a tensor that has to be of that type: for calls beside whose own several types another is easily passed."""
-    assert t is None or t.dtype == dtype, f"{dtype} expected, not {t.dtype}"
-    return _ptr(t)
+def _ptr_of(dtype):
+    """_ptr that takes this type alone: for calls beside whose own several types another is easily passed."""
+    def ptr(t):
+        if t is None:
+            return None
+        assert t.dtype is dtype, f"{dtype} expected, not {t.dtype}"
+        assert t.is_cuda, "device tensor expected"
+        return t.data_ptr()
+    return ptr
 
 
-def _f32(t):
-    return _typed(t, torch.float32)
-
-
-def _i32(t):
-    return _typed(t, torch.int32)
-
-
-def _u8(t):
-    return _typed(t, torch.uint8)
+_f32, _i32, _u8 = _ptr_of(torch.float32), _ptr_of(torch.int32), _ptr_of(torch.uint8)
 
 
 def _stream():
