@@ -14,10 +14,12 @@
 // the CTAs.
 //
 // Two accumulators of up to 224 columns (the epilogue of one tile runs under the products of the next) and four sets of scale factors
-// fill the 512 columns of tensor memory; CTAs of one tile have one accumulator, and two of them fit an SM.
+// fill the 512 columns of tensor memory; CTAs of one tile have one accumulator, and two of them fit an SM.  WIDE (G = 2): one accumulator of
+// up to 416 columns, made by two instructions that share the codes of the columns of C; a quarter less comes from L2 for the same
+// products.  Its epilogue is alone, but the next tile's loads go on under it, and they are the bound.
 //
-// Bound by the way from L2 to the SMs (46 to 54 bytes a cycle) and by power where that is long: 8192^3 with a bf16 result 422 us after a pause
-// (2606 TFLOP/s), 500 in a row at 1.55 GHz; 4096^3 64; one token x 4096 x 4096 7.5, launch and first loads being most of it.
+// Bound by the way from L2 to the SMs (some 40 bytes a cycle for pairs) and by power where that is long: 8192^3 with a bf16 result 404 us
+// (2722 TFLOP/s; 470 on two accumulators), 4096^3 58; one token x 4096 x 4096 7.5, launch and first loads being most of it.
 //
 // Roles per CTA: warp 0 fetches codes (TMA), warp 1 copies scale factors to tensor memory and issues the products, warp 2 brings the
 // scale bytes into the layout they are copied from, warps 4-11 run the epilogue.  Every wait on a barrier is bounded.
@@ -27,11 +29,12 @@
 namespace lpdt {
 namespace tc {
 
-constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleBytes = 1536, kMmScaleSlots = 4, kMmMaxRows = 224 /*2 * 224 + 4 * 16 <= 512*/, kMmRaster = 8;
+constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleSlots = 4, kMmMaxRows = 224 /*2 * 224 + 4 * 16 <= 512*/,
+              kMmWideRows = 416 /*416 + 4 * 20 <= 512*/, kMmRaster = 8;
 constexpr size_t kMmSmem = 227 * 1024;
 
 struct MmParams {
-    int nodes, M, N, kblocks, bn;              // bn: rows of C per tile, a multiple of 16
+    int nodes, M, N, kblocks, bn, bn0;         // bn: rows of C per tile, a multiple of 16; bn0: of the first instruction (WIDE), else bn
     int tilesJ, tilesM, stages, tmem_cols, accs;   // accs: accumulators, 1 where a CTA makes one tile
     int groups, per_cta;                       // SPLIT: groups of 8 rows of a tile that exist, most of them that one CTA adds up
     int slot;                                  // bytes of a stage: codes of both sides
@@ -59,6 +62,9 @@ __device__ __forceinline__ uint32_t mm_peer(uint32_t local, uint32_t rank) {
 }
 __device__ __forceinline__ void mm_arrive_at(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void mm_arrive_relaxed(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 __device__ __forceinline__ void mm_st_peer(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
@@ -118,64 +124,88 @@ __device__ __forceinline__ MmTile mm_tile(const MmParams &p, int tile) {
     return t;
 }
 
-// The rows of scales that a lane brings to tensor memory: of 128 columns of C and 256 rows of it, every 32nd.
-struct MmScaleRows {
-    const uint8_t *row[12];
+// WIDE: a tile's rows are those of two instructions, of bn0 and of bn - bn0 rows, and each CTA holds a half of both: the first half of the
+// tile's rows is one CTA's, the second the other's, and the first bn0 / 2 rows of each half are the first instruction's.  The row of the tile
+// that is column n of the accumulators (which lie side by side).
+__device__ __forceinline__ int mm_wide_row(const MmParams &p, int n) {
+    const bool second = n >= p.bn0;
+    const int i = second ? n - p.bn0 : n, half = (second ? p.bn - p.bn0 : p.bn0) / 2;
+    return (i >= half ? p.bn / 2 + i - half : i) + (second ? p.bn0 / 2 : 0);
+}
+// The rows of scales that a lane brings to tensor memory, every 32nd: of 128 columns of C and of up to 256 rows of it for each instruction.
+// They come in sets of 128 rows, four words a lane.
+template <bool WIDE> struct MmScaleRows {
+    static constexpr int SETS = WIDE ? 5 : 3, BYTES = SETS * 512, COLUMNS = SETS == 3 ? 16 : 20;      // of a slot; columns of tensor memory
+    const uint8_t *row[4 * SETS];
     int sets;
     __device__ __forceinline__ void set(const MmParams &p, const MmTile &t, int G, int rank, int lane) {
-        sets = p.bn > 128 ? 3 : 2;
+        sets = WIDE || p.bn > 128 ? SETS : 2;
         const int j0 = (t.jt * G + (G == 2 ? rank : 0)) * 128, m0 = t.mt * p.bn;
         const uint8_t *b = p.sB + (size_t)t.node * p.N * p.spitch, *a = p.sA + (size_t)t.node * p.M * p.spitch;
 #pragma unroll
-        for (int i = 0; i < 12; ++i) {
-            const int r = (i & 3) * 32 + lane + (i >= 8 ? 128 : 0), at = (i < 4 ? j0 : m0) + r;
-            const bool have = i < 4 ? at < p.N : (r < p.bn && at < p.M);
+        for (int i = 0; i < 4 * SETS; ++i) {
+            const int r = (i & 3) * 32 + lane + (i >= 8 && (i & 4) == 0 ? 128 : 0);      // sets 0; 1, 2; 3, 4
+            const int n = i >= 12 ? p.bn0 + r : r, limit = WIDE && i < 12 ? p.bn0 : p.bn;
+            const int at = i < 4 ? j0 + r : m0 + (WIDE ? mm_wide_row(p, n) : n);
+            const bool have = i < 4 ? at < p.N : (n < limit && at < p.M);
             row[i] = have ? (i < 4 ? b : a) + (size_t)at * p.spitch : nullptr;
         }
     }
-    __device__ __forceinline__ void fetch(uint32_t (&w)[12], int word) const {
+    __device__ __forceinline__ void fetch(uint32_t (&w)[4 * SETS], int word) const {
 #pragma unroll
-        for (int i = 0; i < 12; ++i)
-            w[i] = (i < 8 || sets == 3) && row[i] ? __ldg(reinterpret_cast<const uint32_t *>(row[i]) + word) : 0x7f7f7f7fu;
+        for (int i = 0; i < 4 * SETS; ++i)
+            w[i] = (i < 8 || sets > 2) && row[i] ? __ldg(reinterpret_cast<const uint32_t *>(row[i]) + word) : 0x7f7f7f7fu;
     }
 };
 
-// 16 rows of C from m on, column j of it per lane.
+// 16 rows of C from m on, column j of it per lane: what is added to them, and their storing.
 template <typename OutT>
-__device__ __forceinline__ void mm_store(const MmParams &p, int node, int m, int j, const float (&v)[16], float bias) {
-    if (j >= p.N) return;
-    const long long at = node * p.c_node + m * p.c_row + j;
+__device__ __forceinline__ void mm_addend(const MmParams &p, int node, int m, int j, OutT (&x)[16]) {
+    if (!p.addend || j >= p.N) return;
+    const OutT *a = (const OutT *)p.addend + (node * p.c_node + m * p.c_row + j);
     const int have = p.M - m;
-    float f[16];
+    if (have >= 16) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = v[i];
+        for (int i = 0; i < 16; ++i, a += p.c_row) x[i] = *a;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i, a += p.c_row)
+            if (i < have) x[i] = *a;
+    }
+}
+template <typename OutT>
+__device__ __forceinline__ void mm_store(const MmParams &p, int node, int m, int j, float (&f)[16], float bias, const OutT (&x)[16]) {
+    if (j >= p.N) return;
+    OutT *c = (OutT *)p.C + (node * p.c_node + m * p.c_row + j);
+    const int have = p.M - m;
     if (p.bias) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) f[i] = __fadd_rn(f[i], bias);
     }
     if (p.addend) {
-        const OutT *a = (const OutT *)p.addend + at;
-        float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = i < have ? to_f32(a[i * p.c_row]) : 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = __fadd_rn(f[i], x[i]);
+        for (int i = 0; i < 16; ++i) f[i] = __fadd_rn(f[i], to_f32(x[i]));
     }
-    OutT *c = (OutT *)p.C + at;
+    if (have >= 16) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < have) c[i * p.c_row] = from_f32<OutT>(f[i]);
+        for (int i = 0; i < 16; ++i, c += p.c_row) *c = from_f32<OutT>(f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i, c += p.c_row)
+            if (i < have) *c = from_f32<OutT>(f[i]);
+    }
 }
 
-// SPLIT: the clusters' CTAs share one tile's K (G = 1), a CTA makes one tile.
-template <int G, bool SPLIT, typename OutT>
+// SPLIT: the clusters' CTAs share one tile's K (G = 1), a CTA makes one tile.  WIDE: two instructions side by side (G = 2), one accumulator.
+template <int G, bool SPLIT, bool WIDE, typename OutT>
 __global__ void __launch_bounds__(kMmThreads, G == 1 ? 2 : 1)
 matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const __grid_constant__ CUtensorMap mapR /*A: rows*/, const MmParams p) {
-    static_assert(!(SPLIT && G == 2), "one or the other");
+    static_assert(!(SPLIT && G == 2) && !(WIDE && G == 1), "one or the other");
+    using Rows = MmScaleRows<WIDE>;
     extern __shared__ __align__(1024) unsigned char smem[];
     MmCtl *ctl = reinterpret_cast<MmCtl *>(smem);
     unsigned char *data = smem + 1024, *scales = data + (size_t)p.stages * p.slot;
-    [[maybe_unused]] float *parts = reinterpret_cast<float *>(scales + kMmScaleSlots * kMmScaleBytes);      // SPLIT: [CTA][group][8 rows][128 columns]
+    [[maybe_unused]] float *parts = reinterpret_cast<float *>(scales + kMmScaleSlots * Rows::BYTES);      // SPLIT: [CTA][group][8 rows][128 columns]
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = (G == 2 || SPLIT) ? mm_cluster_rank() : 0u;
     const uint32_t share = SPLIT ? (uint32_t)gridDim.y : 1u;            // gridDim.y = cluster size
@@ -210,8 +240,8 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         }
         pdl_trigger();
     }
-    MmScaleRows rows;
-    uint32_t next[12];
+    Rows rows;
+    uint32_t next[4 * Rows::SETS];
     if (warp == 2) {
         rows.set(p, mm_tile(p, first < total ? first : 0), G, (int)rank, lane);
         pdl_wait();
@@ -255,7 +285,8 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         }
     } else if (warp == 1) {
         if (G == 1 || rank == 0) {
-            const uint32_t idesc = idesc_mx_e4m3(128 * G, p.bn);
+            const uint32_t idesc = idesc_mx_e4m3(128 * G, WIDE ? p.bn0 : p.bn);
+            [[maybe_unused]] const uint32_t idesc1 = idesc_mx_e4m3(128 * G, p.bn - p.bn0);
             const uint64_t tpl = smem_desc(0, 16, 1024, 2), sc_tpl = smem_desc(0, 16, 128, 0);
             const uint32_t sf0 = tmem_base + p.accs * p.bn;
             // Groups of four blocks of K, counted over all tiles: `copied` have their factors in tensor memory or on their way.  A group's are
@@ -270,10 +301,14 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
                 if (!mbar_wait(smem_u32(&ctl->sf_full[slot]), turn & 1, &ctl->abort_flag, p.dev_status)) return false;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t sc = smem_u32(scales + (size_t)slot * kMmScaleBytes) >> 4, sf = sf0 + slot * 16;
+                    const uint32_t sc = smem_u32(scales + (size_t)slot * Rows::BYTES) >> 4, sf = sf0 + slot * Rows::COLUMNS;
                     mm_copy_scales<G>(sf, sc_tpl | (sc & 0x3FFFu));
                     mm_copy_scales<G>(sf + 4, sc_tpl | ((sc + 32) & 0x3FFFu));
-                    if (p.bn > 128) mm_copy_scales<G>(sf + 8, sc_tpl | ((sc + 64) & 0x3FFFu));
+                    if (WIDE || p.bn > 128) mm_copy_scales<G>(sf + 8, sc_tpl | ((sc + 64) & 0x3FFFu));
+                    if constexpr (WIDE) {
+                        mm_copy_scales<G>(sf + 12, sc_tpl | ((sc + 96) & 0x3FFFu));
+                        mm_copy_scales<G>(sf + 16, sc_tpl | ((sc + 128) & 0x3FFFu));
+                    }
                 }
                 __syncwarp();
                 ++copied;
@@ -282,8 +317,8 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             int st = 0; uint32_t ph = 0, tcount = 0;
             bool ok = true;
             for (int tile = first; tile < total && ok && !ctl->abort_flag; tile += step, ++tcount) {
-                const int acc = tcount & 1;
-                if (!mbar_wait(smem_u32(&ctl->tmem_empty[acc]), ((tcount >> 1) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) break;
+                const int acc = WIDE ? 0 : tcount & 1;
+                if (!mbar_wait(smem_u32(&ctl->tmem_empty[acc]), ((WIDE ? tcount : tcount >> 1) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) break;
                 tc_fence_after();
                 for (int kb = k_begin; kb < k_end && ok; ++kb) {
                     const bool fresh = kb == k_begin || (kb & 3) == 0;
@@ -293,11 +328,13 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
                     const uint32_t slot = group & (kMmScaleSlots - 1);
                     const bool last = (kb & 3) == 3 || kb == k_end - 1;
                     if (elect_one()) {
-                        const uint32_t id = idesc | ((uint32_t)(kb & 3) << 4) | ((uint32_t)(kb & 3) << 29), sf = sf0 + slot * 16;
+                        const uint32_t byte = ((uint32_t)(kb & 3) << 4) | ((uint32_t)(kb & 3) << 29), sf = sf0 + slot * Rows::COLUMNS;
                         uint32_t l = smem_u32(data + (size_t)st * p.slot) >> 4, r = l + (kMmLaneBytes >> 4);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            mm_mma<G>(tmem_base + acc * p.bn, tpl | (l & 0x3FFFu), tpl | (r & 0x3FFFu), id, sf, sf + 4, (uint32_t)((kb - k_begin) | k));
+                            mm_mma<G>(tmem_base + acc * p.bn, tpl | (l & 0x3FFFu), tpl | (r & 0x3FFFu), idesc | byte, sf, sf + 4, (uint32_t)((kb - k_begin) | k));
+                            if constexpr (WIDE)
+                                mm_mma<G>(tmem_base + p.bn0, tpl | (l & 0x3FFFu), tpl | ((r + p.bn0 * 4) & 0x3FFFu), idesc1 | byte, sf, sf + 12, (uint32_t)((kb - k_begin) | k));
                             l += 2; r += 2;
                         }
                         mm_commit<G>(smem_u32(&ctl->empty[st]));
@@ -324,14 +361,14 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
             bool ok = true;
             for (int g = k_begin >> 2; g <= last; ++g, ++group) {
                 const int slot = group & (kMmScaleSlots - 1);
-                uint32_t now[12];
+                uint32_t now[4 * Rows::SETS];
 #pragma unroll
-                for (int i = 0; i < 12; ++i) now[i] = next[i];
+                for (int i = 0; i < 4 * Rows::SETS; ++i) now[i] = next[i];
                 if (g < last) rows.fetch(next, g + 1);
                 if (!mbar_wait(smem_u32(&ctl->sf_done[slot]), ((group / kMmScaleSlots) & 1) ^ 1, &ctl->abort_flag, p.dev_status)) { ok = false; break; }
-                uint4 *dst = reinterpret_cast<uint4 *>(scales + (size_t)slot * kMmScaleBytes) + lane;
+                uint4 *dst = reinterpret_cast<uint4 *>(scales + (size_t)slot * Rows::BYTES) + lane;
 #pragma unroll
-                for (int i = 0; i < 3; ++i)
+                for (int i = 0; i < Rows::SETS; ++i)
                     if (i < rows.sets) dst[i * 32] = make_uint4(now[4 * i], now[4 * i + 1], now[4 * i + 2], now[4 * i + 3]);
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -349,24 +386,46 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         const int q = warp & 3, half = (warp - 4) >> 2, chunks = p.bn / 16;
         const uint32_t empty0 = G == 2 ? mm_peer(smem_u32(&ctl->tmem_empty[0]), 0) : smem_u32(&ctl->tmem_empty[0]);
         uint32_t tcount = 0;
+        // This warp's part of the accumulator is in registers.  The loads are complete, and nothing else is handed over; a release would
+        // wait for the stores to C of the whole tile (pairs: 8192 x 8192 x 512 77 us with it).
+        auto done = [&](int acc) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (G == 2) mm_arrive_relaxed(empty0 + acc * 8);
+                else mbar_arrive(empty0 + acc * 8);
+            }
+        };
         pdl_wait();
         if constexpr (SPLIT) mm_cluster_wait();       // the others have started
         for (int tile = first; tile < total && !ctl->abort_flag; tile += step, ++tcount) {
             const MmTile t = mm_tile(p, tile);
             const int j = (t.jt * G + (G == 2 ? (int)rank : 0)) * 128 + q * 32 + lane, m0 = t.mt * p.bn;
             const float bias = p.bias && j < p.N ? p.bias[t.node * p.bias_node + j] : 0.f;
-            const int acc = tcount & 1;
-            if (!mbar_wait(smem_u32(&ctl->tmem_full[acc]), (tcount >> 1) & 1, &ctl->abort_flag, p.dev_status)) break;
+            const int acc = WIDE ? 0 : tcount & 1;
+            if (!mbar_wait(smem_u32(&ctl->tmem_full[acc]), (WIDE ? tcount : tcount >> 1) & 1, &ctl->abort_flag, p.dev_status)) break;
             tc_fence_after();
             const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * p.bn;
+            auto row_of = [&](int c) { return m0 + (WIDE ? mm_wide_row(p, c * 16) : c * 16); };
             uint32_t v[16];
+            OutT next_x[16] = {};
             if (half < chunks) tmem_ld_32x16(t_row + half * 16, v);
+            if (G == 2 && half < chunks) mm_addend<OutT>(p, t.node, row_of(half), j, next_x);
             for (int c = half; c < chunks; c += 2) {
+                OutT x[16] = {};
+                if constexpr (G == 2) {
+                    // what is added to a piece is on its way while the piece before it is stored
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = next_x[i];
+                    if (c + 2 < chunks) mm_addend<OutT>(p, t.node, row_of(c + 2), j, next_x);
+                } else if constexpr (!SPLIT)
+                    mm_addend<OutT>(p, t.node, row_of(c), j, x);
                 tmem_ld_wait();
                 float f[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
                 if (c + 2 < chunks) tmem_ld_32x16(t_row + (c + 2) * 16, v);
+                else done(acc);
                 if constexpr (SPLIT) {
                     // groups of 8 rows go to the CTAs in turn, each to where that CTA keeps this one's
 #pragma unroll
@@ -378,15 +437,10 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
 #pragma unroll
                         for (int i = 0; i < 8; ++i) mm_st_peer(to + i * 512, f[8 * h + i]);
                     }
-                } else if (m0 + c * 16 < p.M)
-                    mm_store<OutT>(p, t.node, m0 + c * 16, j, f, bias);
+                } else if (row_of(c) < p.M)
+                    mm_store<OutT>(p, t.node, row_of(c), j, f, bias, x);
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (G == 2) mm_arrive_at(empty0 + acc * 8);
-                else mbar_arrive(empty0 + acc * 8);
-            }
+            if (half >= chunks) done(acc);
         }
     }
     if constexpr (SPLIT) {
@@ -410,7 +464,9 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
                 }
                 MmParams e = p;
                 if (e.M > m + 8) e.M = m + 8;
-                mm_store<OutT>(e, t.node, m, j, s, bias);
+                OutT x[16] = {};
+                mm_addend<OutT>(e, t.node, m, j, x);
+                mm_store<OutT>(e, t.node, m, j, s, bias, x);
             }
         }
     }
@@ -426,50 +482,60 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     }
 }
 
-struct MmPlan { int g, bn, split, dense; };
+struct MmPlan { int g, bn, split, dense, wide; };
 
 // The least of an estimate in cycles over pairs and single SMs, rows per tile and shares of K.  A block of 128 values of K takes a tile of bn
-// rows the products' 2 * bn cycles or, where that is more, what its codes take from L2: 48 bytes a cycle of an SM by itself, 34 of one of
-// a pair.  An epilogue of some 8 cycles a row runs under the next tile's products, the last one by itself.  Clusters of 8 find room on 96
-// SMs at once.  `dense`: two CTAs of one tile each on an SM instead of one that walks over tiles, where one round of them is enough; one's
-// epilogue then runs beside the other's loads, whose halves of the SM take 24 bytes a cycle each.  (Fitted to every plan's time for 29
-// shapes from 1 x 4096 x 4096 to 4096^3: the plan is within 2 % of the best on average.  Pairs pay for themselves when every SM has
-// several tiles of long K: 4096^3 65.0 us against 67.7 on single SMs, 2048^3 17.6 against 16.0; dense 2048^3 13.3 us; narrow tiles or
-// dense ones would cost many tiles of short K a third: 2 x 4188 x 4744 x 259 42.9 us, 55.4 by a plan without the epilogue's share.)
-static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks) {
-    MmPlan best = {1, 16, 1, 0};
+// rows the products' 2 * bn cycles or, where that is more, what its codes take from L2: 56 bytes a cycle of an SM by itself, 42 of one of
+// a pair, 36 where the pair's tiles are wide.  An epilogue of `row` cycles a row (8, 10 of fp32, 16 with an addend) runs under the next
+// tile's products, the last one by itself; three times that, being alone, behind a wide tile's products, and the next tile's loads go on
+// meanwhile.  Clusters share K where one round of them is enough (a second would wait for whole clusters to end: 2048 x 2048 x 8192 94 us,
+// 34 on wide tiles); those of 8 find room on 96 SMs at once.  `dense`: two CTAs of one tile each on an SM instead of one that walks over
+// tiles, where one round of them is enough; one's epilogue then runs beside the other's loads, 32 bytes a cycle each.  (Fitted to every plan's
+// time for 36 shapes from 1 x 4096 x 4096 to 8192 x 8192 x 16384, each with bf16 and fp32 results and an addend: 1.4 % above the best plan on
+// average.  Wide against pairs of two accumulators: 8192^3 404 us, 470; 8192 x 8192 x 16384 900, 1127; 4096^3 58, 64; short K the other
+// way, 8192 x 8192 x 512 64, 49.  Dense 2048^3 12.7, 14.7 wide, 15.3 on single SMs.)
+static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks, double row) {
+    MmPlan best = {1, 16, 1, 0, 0};
     double least = 1e300;
+    const int64_t rows = (int64_t)align_up((size_t)M, 16);
     for (int g = 1; g <= 2; ++g) {
         const int64_t tj = ceil_div(N, 128 * g);
         for (int bn = 16 * g; bn <= kMmMaxRows; bn += 16 * g) {           // the instruction's column counts: by 16, in pairs by 32
-            if (bn > (int64_t)align_up((size_t)M, 16)) break;
+            if (bn > rows) break;
             const int64_t tiles = (int64_t)nodes * tj * ceil_div(M, bn);
             const double bytes = kMmLaneBytes + bn * 128.0 / g;
-            const double from_l2 = bytes / (g == 1 ? 48 : 34), per = from_l2 > 2.0 * bn ? from_l2 : 2.0 * bn;
+            const double from_l2 = bytes / (g == 1 ? 56 : 42), per = from_l2 > 2.0 * bn ? from_l2 : 2.0 * bn;
             for (int split = 1; split <= (g == 1 && bn <= 128 ? 8 : 1); split *= 2) {
                 if (split > kblocks) break;
-                const int64_t slots = split == 8 ? 96 : kNumSMs / (g * split) * (g * split);
-                const double waves = (double)ceil_div(tiles * g * split, slots), k = ceil_div(kblocks, split) * per;
-                const double cost = split > 1 ? waves * (k + 12.0 * bn) + 900
-                                              : waves * (k + 200 > 8.0 * bn ? k + 200 : 8.0 * bn) + 12.0 * bn + (g == 2 ? 1500 : 0);
-                if (cost < least) { least = cost; best = {g, bn, split, 0}; }
+                const int64_t slots = split == 8 ? 96 : kNumSMs / (g * split) * (g * split), waves = ceil_div(tiles * g * split, slots);
+                if (split > 1 && waves > 1) break;
+                const double k = ceil_div(kblocks, split) * per;
+                const double cost = split > 1 ? k + 12.0 * bn + 900
+                                              : (double)waves * (k + 600 > row * bn ? k + 600 : row * bn) + row / 2 * bn + (g == 2 ? 2000 : 0);
+                if (cost < least) { least = cost; best = {g, bn, split, 0, 0}; }
             }
             if (g == 1 && bn >= 64 && bn <= 128 && tiles > kNumSMs && tiles <= 2 * kNumSMs) {
-                const double shared = bytes / 24 > 4.0 * bn ? bytes / 24 : 4.0 * bn;
-                const double cost = kblocks * shared + 8.0 * bn;
-                if (cost < least) { least = cost; best = {1, bn, 1, 1}; }
+                const double shared = bytes / 32 > 4.0 * bn ? bytes / 32 : 4.0 * bn;
+                const double cost = kblocks * shared + row * bn;
+                if (cost < least) { least = cost; best = {1, bn, 1, 1, 0}; }
             }
         }
+    }
+    for (int bn = 256; bn <= kMmWideRows && (bn <= rows || (bn == 256 && M > kMmMaxRows)); bn += 32) {
+        const int64_t waves = ceil_div((int64_t)nodes * ceil_div(N, 256) * ceil_div(M, bn), kNumSMs / 2);
+        const double loads = kblocks * (kMmLaneBytes + bn * 64.0) / 36 + 500, work = kblocks * 2.0 * bn + 3 * row * bn;
+        const double cost = (double)waves * (loads > work ? loads : work) + row / 2 * bn + 2000;
+        if (cost < least) { least = cost; best = {2, bn, 1, 0, 1}; }
     }
     return best;
 }
 
-template <int G, bool SPLIT, typename OutT>
+template <int G, bool SPLIT, bool WIDE, typename OutT>
 static lpdt_status mm_launch(const CUtensorMap &mL, const CUtensorMap &mR, const MmParams &p, int64_t tiles, int split, size_t smem, cudaStream_t st) {
     static PerDeviceOnce attr;
     int dev;
     if (attr.pending(&dev)) {
-        LPDT_CUDA(cudaFuncSetAttribute(matmul_e4m3_kernel<G, SPLIT, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmSmem));
+        LPDT_CUDA(cudaFuncSetAttribute(matmul_e4m3_kernel<G, SPLIT, WIDE, OutT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMmSmem));
         attr.mark(dev);
     }
     if constexpr (SPLIT) {
@@ -484,10 +550,10 @@ static lpdt_status mm_launch(const CUtensorMap &mL, const CUtensorMap &mR, const
         cfg.attrs = a;
         cfg.numAttrs = pdl_enabled() ? 2 : 1;
         ++g_launch_count;
-        cudaLaunchKernelEx(&cfg, matmul_e4m3_kernel<G, SPLIT, OutT>, mL, mR, p);
+        cudaLaunchKernelEx(&cfg, matmul_e4m3_kernel<G, SPLIT, WIDE, OutT>, mL, mR, p);
     } else {
-        const int64_t ctas = tiles * G < kNumSMs || p.accs == 1 ? tiles * G : kNumSMs;
-        launch_k_cluster(matmul_e4m3_kernel<G, SPLIT, OutT>, (unsigned)ctas, kMmThreads, smem, st, G, mL, mR, p);
+        const int64_t ctas = tiles * G < kNumSMs || (p.accs == 1 && !WIDE) ? tiles * G : kNumSMs;
+        launch_k_cluster(matmul_e4m3_kernel<G, SPLIT, WIDE, OutT>, (unsigned)ctas, kMmThreads, smem, st, G, mL, mR, p);
     }
     LPDT_LAUNCH_CHECK();
     return LPDT_OK;
@@ -514,24 +580,25 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     if (M > limit || N > limit || K > limit) return LPDT_ERR_UNSUPPORTED;
 
     const int64_t kblocks = ceil_div(K, 128), pitch = lpdt_e4m3_pitch(K);
-    const MmPlan plan = mm_plan(nodes, M, N, kblocks);
+    const MmPlan plan = mm_plan(nodes, M, N, kblocks, addend ? 16.0 : c_dtype == LPDT_F32 ? 10.0 : 8.0);
     MmParams p = {};
     p.nodes = nodes; p.M = (int)M; p.N = (int)N; p.kblocks = (int)kblocks; p.bn = plan.bn;
+    p.bn0 = plan.wide ? (int)align_up((size_t)plan.bn / 2, 32) : plan.bn;
     p.tilesJ = (int)ceil_div(N, 128 * plan.g); p.tilesM = (int)ceil_div(M, plan.bn);
     const int64_t tiles = (int64_t)nodes * p.tilesJ * p.tilesM;
     if (tiles > 0x3fffffff) return LPDT_ERR_UNSUPPORTED;
     p.slot = kMmLaneBytes + (int)align_up((size_t)(plan.bn / plan.g) * 128, 1024);
     p.groups = (int)ceil_div(M < plan.bn ? M : plan.bn, 8);
     p.per_cta = (int)ceil_div(p.groups, plan.split);
-    const size_t rest = 1024 + kMmScaleSlots * kMmScaleBytes + (plan.split > 1 ? (size_t)plan.split * p.per_cta * 4096 : 0);
+    const size_t rest = 1024 + kMmScaleSlots * (plan.wide ? MmScaleRows<true>::BYTES : MmScaleRows<false>::BYTES) + (plan.split > 1 ? (size_t)plan.split * p.per_cta * 4096 : 0);
     p.stages = (int)((kMmSmem - rest) / p.slot);
     if (p.stages > kMmMaxStages) p.stages = kMmMaxStages;
     // Few rows: half of an SM's shared memory holds enough of them in flight, and the other half lets the next such call's CTAs start.
     const int half = (int)((kMmSmem / 2 - 1024 - rest) / p.slot);
     if (plan.bn <= 64 && tiles * plan.split <= kNumSMs && half >= 4 && p.stages > half) p.stages = half;
-    p.accs = plan.dense || plan.split > 1 ? 1 : 2;
+    p.accs = plan.dense || plan.wide || plan.split > 1 ? 1 : 2;
     if (plan.dense) p.stages = half;
-    for (p.tmem_cols = 128; p.tmem_cols < p.accs * plan.bn + kMmScaleSlots * 16; p.tmem_cols *= 2) {}
+    for (p.tmem_cols = 128; p.tmem_cols < p.accs * plan.bn + kMmScaleSlots * (plan.wide ? MmScaleRows<true>::COLUMNS : MmScaleRows<false>::COLUMNS); p.tmem_cols *= 2) {}
     p.sA = sA; p.sB = sB; p.spitch = (int)lpdt_e4m3_scale_pitch(K);
     p.bias = bias; p.bias_node = nodes == 1 ? 0 : bias_node_stride;
     p.addend = addend; p.C = C; p.c_node = nodes == 1 ? 0 : c_node_stride; p.c_row = M == 1 ? 0 : c_row_stride;
@@ -547,8 +614,9 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     const cudaStream_t st = as_stream(stream);
     return with_dtype(c_dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
-        if (plan.g == 2) return mm_launch<2, false, T>(mL, mR, p, tiles, 1, smem, st);
-        if (plan.split > 1) return mm_launch<1, true, T>(mL, mR, p, tiles, plan.split, smem, st);
-        return mm_launch<1, false, T>(mL, mR, p, tiles, 1, smem, st);
+        if (plan.wide) return mm_launch<2, false, true, T>(mL, mR, p, tiles, 1, smem, st);
+        if (plan.g == 2) return mm_launch<2, false, false, T>(mL, mR, p, tiles, 1, smem, st);
+        if (plan.split > 1) return mm_launch<1, true, false, T>(mL, mR, p, tiles, plan.split, smem, st);
+        return mm_launch<1, false, false, T>(mL, mR, p, tiles, 1, smem, st);
     });
 }

@@ -160,6 +160,20 @@ def test_matmul(shape, dtype):
         assert ((err <= tol) | (over & (np.abs(got) >= torch.finfo(dtype).max) & (np.sign(got) == np.sign(want)))).all(), (err / tol).max()
 
 
+# wide tiles of pairs: one a pair, several; rows that end in each half of them; several nodes; the last with an addend too
+WIDE = [(2, 231, 6725, 2861), (2, 906, 5701, 1478), (3, 337, 4272, 2094), (3, 747, 5016, 1793), (3, 789, 2479, 2097), (1, 519, 7988, 2962)]
+
+
+@pytest.mark.parametrize("shape", WIDE)
+def test_matmul_in_wide_tiles_is_exact(shape):
+    test_matmul_of_whole_numbers_is_exact(shape)
+
+
+@pytest.mark.parametrize("dtype,shape", [(torch.float32, WIDE[5]), (torch.bfloat16, WIDE[4]), (torch.float16, WIDE[1])])
+def test_matmul_in_wide_tiles(shape, dtype):
+    test_matmul(shape, dtype)
+
+
 @pytest.mark.parametrize("shape", [(2, 37, 100, 256), (1, 300, 515, 640), (3, 1, 64, 2048)])
 def test_matmul_into_a_flat_vector_and_onto_itself(shape):
     """Rows apart from one another inside a flat vector: nothing between them is written; addend = C accumulates."""
