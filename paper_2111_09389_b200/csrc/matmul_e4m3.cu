@@ -493,7 +493,8 @@ struct MmPlan { int g, bn, split, dense, wide; };
 // tiles, where one round of them is enough; one's epilogue then runs beside the other's loads, 32 bytes a cycle each.  (Fitted to every plan's
 // time for 36 shapes from 1 x 4096 x 4096 to 8192 x 8192 x 16384, each with bf16 and fp32 results and an addend: 1.4 % above the best plan on
 // average.  Wide against pairs of two accumulators: 8192^3 404 us, 470; 8192 x 8192 x 16384 900, 1127; 4096^3 58, 64; short K the other
-// way, 8192 x 8192 x 512 64, 49.  Dense 2048^3 12.7, 14.7 wide, 15.3 on single SMs.)
+// way, 8192 x 8192 x 512 64, 49.  Dense 2048^3 12.7, 14.7 wide, 15.3 on single SMs;
+// 1 x 28672 x 4096 23.0, 25.1.)
 static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks, double row) {
     MmPlan best = {1, 16, 1, 0, 0};
     double least = 1e300;
@@ -514,7 +515,7 @@ static MmPlan mm_plan(int nodes, int64_t M, int64_t N, int64_t kblocks, double r
                                               : (double)waves * (k + 600 > row * bn ? k + 600 : row * bn) + row / 2 * bn + (g == 2 ? 2000 : 0);
                 if (cost < least) { least = cost; best = {g, bn, split, 0, 0}; }
             }
-            if (g == 1 && bn >= 64 && bn <= 128 && tiles > kNumSMs && tiles <= 2 * kNumSMs) {
+            if (g == 1 && bn <= 128 && tiles > kNumSMs && tiles <= 2 * kNumSMs) {
                 const double shared = bytes / 32 > 4.0 * bn ? bytes / 32 : 4.0 * bn;
                 const double cost = kblocks * shared + row * bn;
                 if (cost < least) { least = cost; best = {1, bn, 1, 1, 0}; }
@@ -593,9 +594,10 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     const size_t rest = 1024 + kMmScaleSlots * (plan.wide ? MmScaleRows<true>::BYTES : MmScaleRows<false>::BYTES) + (plan.split > 1 ? (size_t)plan.split * p.per_cta * 4096 : 0);
     p.stages = (int)((kMmSmem - rest) / p.slot);
     if (p.stages > kMmMaxStages) p.stages = kMmMaxStages;
-    // Few rows: half of an SM's shared memory holds enough of them in flight, and the other half lets the next such call's CTAs start.
+    // Few rows and short K: half of an SM's shared memory holds enough in flight, and the other half lets the next such call's CTAs start
+    // (1 x 4096 x 4096 7.7 us, 8.1 with all of it; 1 x 8192 x 8192 the other way, 16.7 and 15.4).
     const int half = (int)((kMmSmem / 2 - 1024 - rest) / p.slot);
-    if (plan.bn <= 64 && tiles * plan.split <= kNumSMs && half >= 4 && p.stages > half) p.stages = half;
+    if (plan.bn <= 64 && tiles * plan.split <= kNumSMs && ceil_div(kblocks, plan.split) <= 16 && half >= 4 && p.stages > half) p.stages = half;
     p.accs = plan.dense || plan.wide || plan.split > 1 ? 1 : 2;
     if (plan.dense) p.stages = half;
     for (p.tmem_cols = 128; p.tmem_cols < p.accs * plan.bn + kMmScaleSlots * (plan.wide ? MmScaleRows<true>::COLUMNS : MmScaleRows<false>::COLUMNS); p.tmem_cols *= 2) {}
