@@ -30,7 +30,7 @@ namespace lpdt {
 namespace tc {
 
 constexpr int kMmThreads = 384, kMmMaxStages = 10, kMmLaneBytes = 16384, kMmScaleSlots = 4, kMmMaxRows = 224 /*2 * 224 + 4 * 16 <= 512*/,
-              kMmWideRows = 416 /*416 + 4 * 20 <= 512*/, kMmRaster = 8;
+              kMmWideRows = 416 /*416 + 4 * 20 <= 512*/, kMmRaster = 8, kMmSoon = 8;
 constexpr size_t kMmSmem = 227 * 1024;
 
 struct MmParams {
@@ -42,11 +42,12 @@ struct MmParams {
     int spitch;                                // bytes of a row of scales
     const float *bias; long long bias_node;
     const void *addend;
+    bool early;                                // ask for the addend before a tile's products end
     void *C; long long c_node, c_row;
     int32_t *dev_status;
 };
 struct MmCtl {
-    unsigned long long full[kMmMaxStages], empty[kMmMaxStages], sf_full[kMmScaleSlots], sf_done[kMmScaleSlots], tmem_full[2], tmem_empty[2];
+    unsigned long long full[kMmMaxStages], empty[kMmMaxStages], sf_full[kMmScaleSlots], sf_done[kMmScaleSlots], tmem_full[2], tmem_empty[2], soon[2];
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -63,6 +64,7 @@ __device__ __forceinline__ uint32_t mm_peer(uint32_t local, uint32_t rank) {
 __device__ __forceinline__ void mm_arrive_at(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+__device__ __forceinline__ void mm_prefetch(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ void mm_arrive_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
@@ -214,6 +216,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
     const int k_begin = SPLIT ? (int)((long long)p.kblocks * rank / share) : 0;
     const int k_end = SPLIT ? (int)((long long)p.kblocks * (rank + 1) / share) : p.kblocks;
     const int halfn = p.bn / G;                                         // rows of A per CTA
+    const bool soon = !SPLIT && p.early && p.kblocks > kMmSoon;        // the epilogue hears of a tile's end so many blocks of K before
 
     // Each role waits for the kernels before this one at its first access of global memory, and does what it can before: the fetching warp
     // sets the barriers up and goes on (its loads need nothing else), the scales' warp asks for the first words, meanwhile.
@@ -224,7 +227,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         if (lane == 0) {
             for (int i = 0; i < p.stages; ++i) { mbar_init(smem_u32(&ctl->full[i]), 1); mbar_init(smem_u32(&ctl->empty[i]), 1); }
             for (int i = 0; i < kMmScaleSlots; ++i) { mbar_init(smem_u32(&ctl->sf_full[i]), G); mbar_init(smem_u32(&ctl->sf_done[i]), 1); }
-            for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->tmem_full[i]), 1); mbar_init(smem_u32(&ctl->tmem_empty[i]), 8 * G); }
+            for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&ctl->tmem_full[i]), 1); mbar_init(smem_u32(&ctl->tmem_empty[i]), 8 * G); mbar_init(smem_u32(&ctl->soon[i]), 1); }
             ctl->abort_flag = 0;
             mbar_fence_init();
         }
@@ -339,6 +342,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
                         }
                         mm_commit<G>(smem_u32(&ctl->empty[st]));
                         if (last) mm_commit<G>(smem_u32(&ctl->sf_done[slot]));
+                        if (soon && kb == k_end - 1 - kMmSoon) mm_commit<G>(smem_u32(&ctl->soon[acc]));
                         if (kb == k_end - 1) mm_commit<G>(smem_u32(&ctl->tmem_full[acc]));
                     }
                     __syncwarp();
@@ -401,12 +405,28 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         for (int tile = first; tile < total && !ctl->abort_flag; tile += step, ++tcount) {
             const MmTile t = mm_tile(p, tile);
             const int j = (t.jt * G + (G == 2 ? (int)rank : 0)) * 128 + q * 32 + lane, m0 = t.mt * p.bn;
+            auto row_of = [&](int c) { return m0 + (WIDE ? mm_wide_row(p, c * 16) : c * 16); };
             const float bias = p.bias && j < p.N ? p.bias[t.node * p.bias_node + j] : 0.f;
             const int acc = WIDE ? 0 : tcount & 1;
-            if (!mbar_wait(smem_u32(&ctl->tmem_full[acc]), (WIDE ? tcount : tcount >> 1) & 1, &ctl->abort_flag, p.dev_status)) break;
+            const uint32_t phase = (WIDE ? tcount : tcount >> 1) & 1;
+            if constexpr (!SPLIT) {
+                // what will be added comes to L2 under the last products (any earlier, and long K would drive it out again)
+                if (p.early) {
+                    if (soon && !mbar_wait(smem_u32(&ctl->soon[acc]), phase, &ctl->abort_flag, p.dev_status)) break;
+                    const OutT *a = (const OutT *)p.addend + (t.node * p.c_node + (j - lane));
+                    const int last = p.N - 1 - (j - lane);
+                    for (int r = lane; r < (chunks - half + 1) / 2 * 16; r += 32) {
+                        const int m = row_of(half + r / 16 * 2) + r % 16;
+                        if (m < p.M && last >= 0) {
+                            mm_prefetch(a + m * p.c_row);
+                            mm_prefetch(a + m * p.c_row + (last < 31 ? last : 31));
+                        }
+                    }
+                }
+            }
+            if (!mbar_wait(smem_u32(&ctl->tmem_full[acc]), phase, &ctl->abort_flag, p.dev_status)) break;
             tc_fence_after();
             const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + acc * p.bn;
-            auto row_of = [&](int c) { return m0 + (WIDE ? mm_wide_row(p, c * 16) : c * 16); };
             uint32_t v[16];
             OutT next_x[16] = {};
             if (half < chunks) tmem_ld_32x16(t_row + half * 16, v);
@@ -605,6 +625,9 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
     p.bias = bias; p.bias_node = nodes == 1 ? 0 : bias_node_stride;
     p.addend = addend; p.C = C; p.c_node = nodes == 1 ? 0 : c_node_stride; p.c_row = M == 1 ? 0 : c_row_stride;
     p.dev_status = dev_status;
+    // Where the epilogue is not hidden: behind wide tiles (8192^3 fp32 553 -> 540 us), short K (8192 x 8192 x 512 fp32 138 -> 112) or a CTA's only
+    // tile (512 x 4096 x 4096 fp32 17.8 -> 16.9).  Elsewhere it only disturbs the loads: 16384 x 4096 x 4096 fp32 257 us, 280 with it.
+    p.early = addend && (plan.wide || kblocks <= kMmSoon || tiles * plan.g <= kNumSMs || p.accs == 1);
 
     CUtensorMap mL, mR;
     const uint64_t dL[3] = {(uint64_t)K, (uint64_t)N, (uint64_t)nodes}, sL[2] = {(uint64_t)pitch, (uint64_t)N * pitch};
