@@ -206,9 +206,9 @@ __device__ __noinline__ unsigned long long exact_floor(const Row<T> r, int end, 
     __syncthreads();
     return s_floor;
 }
-// The k best of words [begin, end) and perhaps the edges, in order, from the threads' best turns.  A floor comes first: with M = ceil(k / warps), the least of
-// the warps' M-th largest maxima; each warp has M lanes that reach it, so k values do.  Where many more do (ties: masked rows),
-// a better floor takes less time than ranking them.
+// The k best of words [begin, end) and perhaps the edges, in order, from the threads' best turns.  A floor comes first: with
+// M = ceil(k / warps), the least of the warps' M-th largest maxima; each warp has M lanes that reach it, so k values do.  Where many more
+// do (ties: masked rows), a better floor takes less time than ranking them.
 template <typename T, int TH>
 __device__ __noinline__ void top_of_words(const Row<T> r, int begin, int end, bool edges, const Best b, int k, TopList<TH> &l) {
     __shared__ uint32_t s_least[TH / 32];
