@@ -217,6 +217,51 @@ def test_matmul_at_the_ends_of_the_scales(ea, eb):
         assert np.array_equal(C.double().cpu().numpy(), want)
 
 
+def test_two_streams_at_once_give_the_same_bits():
+    """Products of every form (shared K, one and two tiles an SM, pairs, wide tiles) side by side on two streams, and captured into two graphs."""
+    shapes = [(1, 1, 4096, 4096), (1, 1025, 2049, 300), (2, 700, 1500, 1200), (3, 433, 4791, 2776), (2, 906, 5701, 1478), (1, 64, 4096, 2048)]
+    rng = torch.Generator(device="cuda").manual_seed(3)
+    sets = []
+    for n, M, N, K in shapes:
+        f = []
+        for r in (M, N):
+            x = torch.randn(n, r, K, generator=rng, device="cuda", dtype=torch.float32)
+            q = torch.empty(n, r, api.lpdt_e4m3_pitch(K), dtype=torch.uint8, device="cuda")
+            s = torch.empty(n, r, api.lpdt_e4m3_scale_pitch(K), dtype=torch.uint8, device="cuda")
+            api.lpdt_quantize_e4m3(x, n, r, K, q, s)
+            f += [q, s]
+        C = [torch.empty(n, M, N, dtype=torch.bfloat16, device="cuda") for _ in range(5)]
+        api.lpdt_matmul_e4m3(n, M, N, K, *f, C[0])
+        sets.append(((n, M, N, K), f, C))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    order = (list(range(6)), [4, 0, 5, 2, 1, 3])
+    for rep in range(3):
+        for step in range(6):
+            for i, stream in enumerate(streams):
+                shape, f, C = sets[order[i][step]]
+                with torch.cuda.stream(stream):
+                    api.lpdt_matmul_e4m3(*shape, *f, C[1 + i], dev_status=status)
+    graphs = []
+    for i, stream in enumerate(streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            for k in order[i]:
+                shape, f, C = sets[k]
+                api.lpdt_matmul_e4m3(*shape, *f, C[3 + i], dev_status=status)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for rep in range(2):
+        for g, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                g.replay()
+    torch.cuda.synchronize()
+    assert api.lpdt_check_status(status) == 0
+    for _, _, C in sets:
+        assert all(torch.equal(C[0], c) for c in C[1:])
+
+
 def test_three_products_of_a_layer():
     """Forward, backward-data and backward-weight from the quantizer's two forms, as a layer uses them."""
     g = torch.Generator().manual_seed(0)
