@@ -152,17 +152,19 @@ def _distill(st):
         rest = torch.zeros_like(t[:, :1])
         logt = torch.log(t)
     loss = torch.where(t > 0, t * (logt - (z.gather(1, at) - lse).double()), 0.0).sum(-1, keepdim=True)
-    total = (t.sum(-1, keepdim=True) + rest).float()
-    d = torch.exp(z - lse) * total
-    d.scatter_add_(1, at, -t.float())
-    if st["tail"]:
+    total, outside = t.sum(-1, keepdim=True), 0.0
+    if st["tail"]:                                                    # one more class, where any token is outside the list
         zr = torch.where(listed_, -math.inf, z)
         mr = zr.amax(-1, keepdim=True).clamp(min=-3e38)
         sr = torch.exp(zr - mr).sum(-1, keepdim=True)
         lse_r = mr + torch.log(sr)
         some = (rest > 0) & (sr > 0)
         loss += torch.where(some, rest * (torch.log(rest) - (lse_r - lse).double()), 0.0)
-        d -= torch.where(some & ~listed_, rest.float() * torch.exp(z - lse_r), 0.0)
+        total = total + torch.where(some, rest, 0.0)
+        outside = torch.where(some & ~listed_, rest.float() * torch.exp(z - lse_r), 0.0)
+    d = torch.exp(z - lse) * total.float()
+    d.scatter_add_(1, at, -t.float())
+    d -= outside
     w = st["row_weight"].unsqueeze(1)
     loss = torch.where(w != 0, loss, 0.0)
     d = torch.where(w != 0, d * (w / (st["B"] * st["temperature"])), 0.0)
