@@ -670,9 +670,10 @@ lpdt_status lpdt_token_logprobs_bwd(int64_t rows, int32_t V, const void *logits,
  *   tail = 1: t_j = e^teacher_logprob[j];  what the list leaves, t_R = max(0, 1 - sum t), is one more class, which the
  *             student gives p_R = sum of p over the tokens that are not listed:
  *             L = sum_j t_j (ln t_j - ln p[index j]) + t_R (ln t_R - ln p_R)
+ *             (t_R = 0, in the gradient too, where no token outside the list has a probability)
  *   tail = 0: t = softmax of teacher_logprob over the list (so any additive constant is free; a list of nothing but
  *             -inf has no target: loss and gradient 0), no last term
- * (0 ln 0 = 0; with nothing outside the list the last term is left out).  With t_v the sum over the entries of token v,
+ * (0 ln 0 = 0).  With t_v the sum over the entries of token v,
  *   dL/dlogits[v] = (p[v] (sum t + t_R) - t_v) / temperature                    for listed v
  *                   (p[v] (sum t + t_R) - t_R p[v] / p_R) / temperature         for the others
  * row_loss[n][b] = L;  loss[n] = sum_b row_weight L / B;  dlogits = row_weight / B * dL/dlogits, the gradient of the loss.
