@@ -640,7 +640,8 @@ lpdt_status lpdt_softmax_ce(int32_t nodes, int32_t B, int32_t K, const float *lo
  *
  * logits : `dtype` (fp32, bf16 or fp16), row r at r*row_stride, V of them;  z = logits / temperature (1e-30 to 1e30).
  * Sums are held in fp32 relative to the row's running maximum and joined with the rest in double.  -inf marks a token that
- * has no probability.  A row that holds a NaN or +inf answers NaN.  Rows may start at any element (16-byte accesses inside).
+ * has no probability.  A row that holds a NaN or +inf answers NaN, whatever else it holds.  Rows may start at any element
+ * (16-byte accesses inside).
  *
  * lpdt_token_logprobs
  *   lse[r] = ln sum_v e^z;  logprob[r] = z[tokens[r]] - lse[r];  entropy[r] = -sum_v p ln p, p = e^(z - lse) (0 ln 0 = 0)

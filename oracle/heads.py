@@ -145,6 +145,6 @@ def distill_topk(logits, value, index, tail, temperature=1.0, row_weight=None):
                 if left > 0 and mass > 0:
                     loss += left * np.log(left / mass)
                     g += left * (p - np.where(rest, p / mass, 0))
-            row_loss[n, b] = loss
+            row_loss[n, b] = np.nan if np.isnan(p).any() else loss         # NaN or +inf in the row: also without a list
             grad[n, b] = g * w[n, b] / (B * temperature)
     return (row_loss * w).mean(1), row_loss, grad

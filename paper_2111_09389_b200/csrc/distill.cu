@@ -92,7 +92,8 @@ __device__ __forceinline__ void make_list(const DistillArgs &a, long long row, L
 
 // What a row's gradient comes from once the sums are known: st over the tokens outside the list, sl over those on it, each once.  Only
 // sums and quotients: m is the larger maximum, all the sum relative to it.  left: the teacher's mass outside the list; rest: the factor of
-// 2^((x - st.m) c) there.  A student's row of nothing but mask values (lse below -1e30) has neither loss nor gradient.
+// 2^((x - st.m) c) there.  A student's row of nothing but mask values (lse below -1e30) has neither loss nor gradient.  Maxima pass NaN
+// over, so one among mask values shows in the sums alone: `all` is NaN then, and so are the row's loss and every gradient.
 struct RowTerms { double left, total /* sum t + left */, all; float m, rest; bool outside, masked; };
 __device__ __forceinline__ RowTerms row_terms(const DistillArgs &a, double sum, const Stats &st, const Stats &sl, double g) {
     RowTerms r;
@@ -104,8 +105,8 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs &a, double sum, 
     r.all = from_rest + from_list;
     r.left = a.tail && r.outside ? fmax(1.0 - sum, 0.0) : 0.0;
     r.total = sum + r.left;
-    r.masked = (!r.outside && !inside) || (double)r.m * a.inv_t < -1e30;
-    r.rest = r.outside && !r.masked ? (float)(g * (r.total * (from_rest / r.all) - r.left) / (double)st.s) : 0.f;
+    r.masked = r.all == r.all && ((!r.outside && !inside) || (double)r.m * a.inv_t < -1e30);
+    r.rest = r.masked ? 0.f : r.outside ? (float)(g * (r.total * (from_rest / r.all) - r.left) / (double)st.s) : (float)(0.0 * r.all);
     return r;
 }
 // The loss, by one warp; its three logarithms are one computation on three lanes.  ln of the student's mass outside the list is taken
@@ -119,7 +120,7 @@ __device__ __forceinline__ double row_loss(const DistillArgs &a, const List<K> &
         if (l.t[j] != 0.0) loss += l.t[j] * (l.logt[j] - (((double)l.x[j] - (double)r.m) * a.inv_t - log_all));
     loss = warp_sum(loss);
     if (r.left != 0.0) loss += r.left * (log_left - (((double)st.m - (double)r.m) * a.inv_t + log_out - log_all));
-    return r.masked ? 0.0 : loss;
+    return r.masked ? 0.0 : loss + 0.0 * r.all;                 // (a list without any mass: NaN all the same)
 }
 // The gradient of listed entry j's token, whose teacher's probability is that of all entries of it (`twice`: some token has several).
 template <int K>

@@ -408,6 +408,35 @@ def test_distill_of_rows_with_nan(V):
     assert torch.isnan(d[0, 1:4]).all() and torch.isfinite(d[0, [0, 4]]).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("V,B", [(10, 6), (700, 6), (1024, 40), (3000, 6), (3000, 170), (50000, 6)])
+def test_distill_of_rows_with_nan_beside_masks(V, B, tail, dtype):
+    """One token allowed and its logit NaN or +inf, listed or not, masks of -inf or of the type's lowest value around it, with a list or
+    without any: loss and gradient of the row are NaN, other rows are as they were.  A weight of 0 leaves the row out."""
+    x = logits_of(B, V, dtype, V).view(1, B, V)
+    value, index = lists_of(1, B, V, 4, V)
+    index[0, :, :] = [1, 3, 4, 5]
+    weight = np.ones((1, B), np.float32)
+    low = torch.finfo(dtype).min
+    for row in range(1, B - 1):
+        bad = float("nan") if row % 3 else float("inf")
+        x[0, row] = low if row % 2 else -float("inf")
+        x[0, row, (1, V - 1)[row // 2 % 2]] = bad
+        if row % 5 == 4:
+            index[0, row] = -1
+        if row % 8 == 7:
+            weight[0, row] = 0
+    loss, row_loss, d, _ = distill(x, value, index, tail, weight)
+    bad = np.arange(B) % 8 != 7
+    bad[[0, -1]] = False
+    assert np.array_equal(torch.isnan(row_loss[0]).cpu().numpy(), bad) and torch.isnan(loss).all()
+    assert torch.isnan(d[0, torch.from_numpy(bad).cuda()]).all()
+    L, R, G = heads.distill_topk(x.double().numpy(), value, index, tail, 1.0, weight)
+    within(row_loss, R, 9 * SUM(V) + 2 * U * np.abs(R))
+    within(d, G, 9 * SUM(V) / B + torch.finfo(dtype).eps / 2 * np.abs(G) + 2.0 ** -25)
+
+
 def test_distill_against_differences():
     """Central differences of the loss itself (step 2^-4, third derivatives below 1)."""
     V, k, step = 9, 3, 2.0 ** -4

@@ -63,3 +63,18 @@ def test_gradient_where_nothing_lies_outside_the_list(masked):
         down[0, 0, v] -= 1e-5
         f = lambda x: heads.distill_topk(x, value, index, True)[0][0]
         assert abs((f(up) - f(down)) / 2e-5 - grad[0, 0, v]) < 1e-8
+
+
+@pytest.mark.parametrize("mask", [-np.inf, float(np.finfo(np.float32).min)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_a_row_with_nan_beside_masks_answers_nan(mask, bad):
+    """In the oracle: loss and gradient, with the token on the list, beside it, and without a list; not with a weight of 0."""
+    x = np.full((1, 4, 6), mask)
+    x[0, 0, 2] = x[0, 1, 5] = x[0, 2, 5] = x[0, 3, 2] = bad
+    index = np.array([[[2, 4], [2, 4], [-1, -1], [2, 4]]])
+    value = np.log(np.full((1, 4, 2), 0.3))
+    weight = np.array([[1.0, 1.0, 1.0, 0.0]])
+    for tail in (True, False):
+        _, row_loss, grad = heads.distill_topk(x, value, index, tail, 1.0, weight)
+        assert np.isnan(row_loss[0, :3]).all() and np.isnan(grad[0, :3]).all()
+        assert row_loss[0, 3] == 0 and not grad[0, 3].any()
