@@ -671,7 +671,7 @@ lpdt_status lpdt_token_logprobs_bwd(int64_t rows, int32_t V, const void *logits,
  *   tail = 1: t_j = e^teacher_logprob[j];  what the list leaves, t_R = max(0, 1 - sum t), is one more class, which the
  *             student gives p_R = sum of p over the tokens that are not listed:
  *             L = sum_j t_j (ln t_j - ln p[index j]) + t_R (ln t_R - ln p_R)
- *             (t_R = 0, in the gradient too, where no token outside the list has a probability)
+ *             (t_R = 0, in the gradient too, where the list leaves nothing but mask values: ln p_R + lse < -1e30)
  *   tail = 0: t = softmax of teacher_logprob over the list (so any additive constant is free; a list of nothing but
  *             -inf has no target: loss and gradient 0), no last term
  * (0 ln 0 = 0).  With t_v the sum over the entries of token v,

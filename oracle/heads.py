@@ -141,10 +141,11 @@ def distill_topk(logits, value, index, tail, temperature=1.0, row_weight=None):
                 rest = np.ones(V, bool)
                 rest[ids] = False
                 left = max(0.0, 1 - t.sum()) if tail else 0.0
-                mass = p[rest].sum()
-                if left > 0 and mass > 0:
-                    loss += left * np.log(left / mass)
-                    g += left * (p - np.where(rest, p / mass, 0))
+                # the others' class by its own logarithm, which does not run out where its mass would; mask values have none
+                if left > 0 and rest.any() and not z[n, b, rest].max() < -1e30:
+                    log_mass = np.logaddexp.reduce(logp[rest])
+                    loss += left * (np.log(left) - log_mass)
+                    g += left * (p - np.exp(np.where(rest, logp - log_mass, -np.inf)))
             row_loss[n, b] = np.nan if np.isnan(p).any() else loss         # NaN or +inf in the row: also without a list
             grad[n, b] = g * w[n, b] / (B * temperature)
     return (row_loss * w).mean(1), row_loss, grad

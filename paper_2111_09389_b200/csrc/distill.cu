@@ -92,12 +92,13 @@ __device__ __forceinline__ void make_list(const DistillArgs &a, long long row, L
 
 // What a row's gradient comes from once the sums are known: st over the tokens outside the list, sl over those on it, each once.  Only
 // sums and quotients: m is the larger maximum, all the sum relative to it.  left: the teacher's mass outside the list; rest: the factor of
-// 2^((x - st.m) c) there.  A student's row of nothing but mask values (lse below -1e30) has neither loss nor gradient.  Maxima pass NaN
-// over, so one among mask values shows in the sums alone: `all` is NaN then, and so are the row's loss and every gradient.
+// 2^((x - st.m) c) there.  A list that leaves nothing but mask values (-inf, or finite and their lse below -1e30) leaves no class of
+// others.  A student's row of nothing but mask values has neither loss nor gradient.  Maxima pass NaN over, so one among mask values shows in
+// the sums alone: `all` is NaN then, and so are the row's loss and every gradient.
 struct RowTerms { double left, total /* sum t + left */, all; float m, rest; bool outside, masked; };
 __device__ __forceinline__ RowTerms row_terms(const DistillArgs &a, double sum, const Stats &st, const Stats &sl, double g) {
     RowTerms r;
-    r.outside = !(st.s == 0.f);
+    r.outside = !(st.s == 0.f || (st.s == st.s && (double)st.m * a.inv_t < -1e30));
     const bool inside = !(sl.s == 0.f);
     r.m = r.outside && inside ? fmaxf(st.m, sl.m) : r.outside ? st.m : sl.m;
     const double from_rest = r.outside ? (double)st.s * (double)ex2(max_nan((st.m - r.m) * a.c, kFar)) : 0.0;

@@ -437,6 +437,45 @@ def test_distill_of_rows_with_nan_beside_masks(V, B, tail, dtype):
     within(d, G, 9 * SUM(V) / B + torch.finfo(dtype).eps / 2 * np.abs(G) + 2.0 ** -25)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,B", [(10, 5), (700, 5), (1024, 40), (3000, 5), (3000, 170), (50001, 5)])
+def test_distill_with_masks_of_the_lowest_value(V, B, dtype):
+    """Every token outside the list masked by the type's lowest value: no class of others, as with -inf; some of them masked: those count
+    for nothing.  Listed and masked: a loss near the largest floats or beyond."""
+    x = logits_of(B, V, dtype, V).view(1, B, V)
+    value, index = lists_of(1, B, V, 4, V)
+    low = torch.finfo(dtype).min
+    for row in range(B):
+        rest = np.setdiff1d(np.arange(V), index[0, row])
+        if row % 4 == 0:
+            x[0, row, rest] = low
+        elif row % 4 == 1:
+            x[0, row, rest[::2]] = low
+        elif row % 4 == 2:
+            x[0, row, index[0, row, 2]] = low
+    for tail in (True, False):
+        check_distill(x, value, index, tail)
+
+
+@pytest.mark.parametrize("V", [10, 700, 3000, 50001])
+def test_distill_of_students_far_from_the_others(V):
+    """The tokens outside the list 300 to 5000 below it: ln p_R counts, however little p_R is."""
+    B, k = 5, 4
+    x = logits_of(B, V, torch.float32, V).view(1, B, V)
+    value, index = lists_of(1, B, V, k, V)
+    for row in range(B):
+        x[0, row, index[0, row]] += (300, 1000, 2000, 5000, 0)[row]
+    _, row_loss, d, _ = distill(x, value, index)
+    _, R, G = heads.distill_topk(x.double().numpy(), value, index, True)
+    logp, _ = heads._log_softmax(x.double().numpy())
+    inside = np.zeros(x.shape, bool)
+    np.put_along_axis(inside, index.astype(np.int64), True, -1)
+    rest = np.where(inside, -np.inf, logp)
+    share = np.exp(rest - np.logaddexp.reduce(rest, -1, keepdims=True))      # p / p_R
+    within(row_loss, R, 6 * SUM(V) + 2 * U * np.abs(R))
+    within(d, G, (2 * SUM(V) + 450 * U) * (np.exp(logp) * 2 + share) / B + U * np.abs(G) + 1e-37)      # as in check_distill
+
+
 def test_distill_against_differences():
     """Central differences of the loss itself (step 2^-4, third derivatives below 1)."""
     V, k, step = 9, 3, 2.0 ** -4

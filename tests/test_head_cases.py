@@ -78,3 +78,16 @@ def test_a_row_with_nan_beside_masks_answers_nan(mask, bad):
         _, row_loss, grad = heads.distill_topk(x, value, index, tail, 1.0, weight)
         assert np.isnan(row_loss[0, :3]).all() and np.isnan(grad[0, :3]).all()
         assert row_loss[0, 3] == 0 and not grad[0, 3].any()
+
+
+def test_the_others_class_far_below_the_list():
+    """ln p_R = -1000 has a loss and a gradient though p_R itself is no number in 64 bits; mask values, -inf or finite, have neither."""
+    x = np.array([[[0.0, 0.0, -1000.0, -1000.0]]])
+    value, index = np.log(np.array([[[0.3, 0.3]]])), np.array([[[0, 1]]])
+    loss, _, grad = heads.distill_topk(x, value, index, True)
+    assert np.allclose(loss, 0.6 * np.log(0.6) + 0.4 * (np.log(0.4) + 1000 - np.log(2) + np.log(2)) - 0.6 * np.log(0.5) - 0.6 * np.log(2))
+    assert np.allclose(grad[0, 0], [0.2, 0.2, -0.2, -0.2])
+    for mask in (-np.inf, float(np.finfo(np.float32).min), -2e30):
+        x[0, 0, 2:] = mask
+        loss, _, grad = heads.distill_topk(x, value, index, True)
+        assert np.allclose(loss, 0.6 * (np.log(0.3) + np.log(2))) and np.allclose(grad[0, 0], [0, 0, 0, 0])
