@@ -288,6 +288,7 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         }
     } else if (warp == 1) {
         if (G == 1 || rank == 0) {
+            pdl_wait();               // the limits of the waits below are for this kernel's own loads, not for the kernels before it
             const uint32_t idesc = idesc_mx_e4m3(128 * G, WIDE ? p.bn0 : p.bn);
             [[maybe_unused]] const uint32_t idesc1 = idesc_mx_e4m3(128 * G, p.bn - p.bn0);
             const uint64_t tpl = smem_desc(0, 16, 1024, 2), sc_tpl = smem_desc(0, 16, 128, 0);
