@@ -63,10 +63,11 @@ typedef struct {
 
 const char *lpdt_version(void);
 const char *lpdt_status_string(lpdt_status s);
-/* Name of the contraction kernel that the most recent lpdt_qconv_* call of the calling host thread
- * launched ("" before the first one): the tensor-core pixel-tile, halo-tile or weight-gradient kernel, or
- * a CUDA-core kernel.  For labelling timings; the choice depends on the shape, the alignment and on which
- * outputs were asked for. */
+/* Name of the contraction kernel that the most recent lpdt_qconv_* or lpdt_matmul_e4m3 call of the calling host thread
+ * launched ("" before the first one): the tensor-core pixel-tile, halo-tile or weight-gradient kernel, a CUDA-core
+ * kernel, or the product's kernel with the form it took (single SMs, two tiles an SM, K shared by 2 to 8 CTAs, pairs of SMs
+ * with two accumulators, or with one of so many rows).  For labelling timings; the choice depends on the shape, the
+ * alignment and on which outputs were asked for. */
 const char *lpdt_last_kernel(void);
 /* Number of kernels the calling host thread has enqueued through this library so far (memsets and
  * copies not counted; a launch recorded during stream capture counts once, its replays do not). */

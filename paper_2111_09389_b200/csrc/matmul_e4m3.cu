@@ -504,6 +504,16 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
 }
 
 struct MmPlan { int g, bn, split, dense, wide; };
+// What lpdt_last_kernel answers.
+static const char *mm_name(const MmPlan &plan) {
+    static const char *const wide[] = {"lpdt::tc::matmul_e4m3_kernel<pairs, 256 rows>", "lpdt::tc::matmul_e4m3_kernel<pairs, 288 rows>",
+                                       "lpdt::tc::matmul_e4m3_kernel<pairs, 320 rows>", "lpdt::tc::matmul_e4m3_kernel<pairs, 352 rows>",
+                                       "lpdt::tc::matmul_e4m3_kernel<pairs, 384 rows>", "lpdt::tc::matmul_e4m3_kernel<pairs, 416 rows>"};
+    if (plan.wide) return wide[(plan.bn - 256) / 32];
+    if (plan.g == 2) return "lpdt::tc::matmul_e4m3_kernel<pairs>";
+    if (plan.split > 1) return plan.split == 2 ? "lpdt::tc::matmul_e4m3_kernel<K by 2>" : plan.split == 4 ? "lpdt::tc::matmul_e4m3_kernel<K by 4>" : "lpdt::tc::matmul_e4m3_kernel<K by 8>";
+    return plan.dense ? "lpdt::tc::matmul_e4m3_kernel<two an SM>" : "lpdt::tc::matmul_e4m3_kernel<single>";
+}
 
 // The least of an estimate in cycles over pairs and single SMs, rows per tile and shares of K.  A block of 128 values of K takes a tile of bn
 // rows the products' 2 * bn cycles or, where that is more, what its codes take from L2: 56 bytes a cycle of an SM by itself, 42 of one of
@@ -638,11 +648,13 @@ extern "C" lpdt_status lpdt_matmul_e4m3(int32_t nodes, int64_t M, int64_t N, int
         return LPDT_ERR_CUDA;
     const size_t smem = rest + (size_t)p.stages * p.slot;
     const cudaStream_t st = as_stream(stream);
-    return with_dtype(c_dtype, [&](auto t) -> lpdt_status {
+    const lpdt_status s = with_dtype(c_dtype, [&](auto t) -> lpdt_status {
         using T = decltype(t);
         if (plan.wide) return mm_launch<2, false, true, T>(mL, mR, p, tiles, 1, smem, st);
         if (plan.g == 2) return mm_launch<2, false, false, T>(mL, mR, p, tiles, 1, smem, st);
         if (plan.split > 1) return mm_launch<1, true, false, T>(mL, mR, p, tiles, plan.split, smem, st);
         return mm_launch<1, false, false, T>(mL, mR, p, tiles, 1, smem, st);
     });
+    if (s == LPDT_OK) g_last_kernel = mm_name(plan);
+    return s;
 }

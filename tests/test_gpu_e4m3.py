@@ -174,6 +174,51 @@ def test_matmul_in_wide_tiles(shape, dtype):
     test_matmul(shape, dtype)
 
 
+# The forms that a product takes, each with the kernel that has to answer: tiles of one turn and of several, K above and up to 8 blocks (from
+# where on the epilogue asks for the addend early), results of 4 and 2 bytes.
+F32, BF16, F16 = DTYPES
+FORMS = [
+    ((3, 131, 6709, 1167), F32, True, "<single>"), ((3, 298, 4144, 16), F32, True, "<single>"), ((2, 1, 5698, 1064), BF16, True, "<single>"),
+    ((2, 231, 6725, 2861), F32, True, "<two an SM>"), ((3, 3, 6966, 17), F16, True, "<two an SM>"),
+    ((1, 64, 9000, 8192), F32, True, "<K by 2>"), ((1, 1, 6265, 1595), F16, True, "<K by 2>"), ((1, 1, 5149, 477), F32, False, "<K by 2>"),
+    ((1, 1, 2442, 1753), F32, True, "<K by 4>"), ((1, 1, 1530, 914), BF16, True, "<K by 8>"), ((1, 3, 253, 1176), F32, True, "<K by 8>"),
+    ((3, 219, 3321, 3829), F32, False, "<pairs>"), ((1, 8192, 4096, 1024), F32, True, "<pairs>"), ((2, 1500, 5000, 1024), F32, True, "<pairs>"),
+    ((3, 211, 7953, 1734), F32, True, "<pairs>"), ((2, 3585, 7531, 137), BF16, False, "<pairs>"), ((3, 2095, 2193, 773), F16, True, "<pairs>"),
+    ((2, 493, 7097, 3142), F32, True, "<pairs, 256 rows>"), ((3, 715, 3962, 1367), BF16, False, "<pairs, 256 rows>"),
+    ((2, 2742, 1576, 3853), F32, True, "<pairs, 288 rows>"), ((1, 4779, 1979, 2215), F32, False, "<pairs, 288 rows>"), ((1, 519, 7988, 2962), F32, True, "<pairs, 288 rows>"),
+    ((3, 950, 3747, 3111), F32, True, "<pairs, 320 rows>"), ((2, 906, 5701, 1478), F16, False, "<pairs, 320 rows>"),
+    ((2, 2717, 2206, 3497), F32, True, "<pairs, 352 rows>"), ((3, 337, 4272, 2094), BF16, False, "<pairs, 352 rows>"),
+    ((1, 1816, 6331, 4177), F32, True, "<pairs, 384 rows>"), ((3, 747, 5016, 1793), F16, False, "<pairs, 384 rows>"),
+    ((3, 4663, 923, 3930), F32, True, "<pairs, 416 rows>"), ((1, 2375, 5813, 2332), F32, False, "<pairs, 416 rows>"), ((3, 789, 2479, 2097), BF16, False, "<pairs, 416 rows>")]
+
+
+@pytest.mark.parametrize("shape,dtype,addend,form", FORMS)
+def test_matmul_takes_each_form_and_is_exact(shape, dtype, addend, form):
+    """Whole numbers: sums below 2^24 in fp32 whatever the order, then the one rounding to the type of C.  With an addend into another matrix
+    and onto itself."""
+    nodes, M, N, K = shape
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    codes = torch.from_numpy(heads.e4m3_encode(np.arange(-4.0, 5.0))).cuda()
+    P, S, nb = api.lpdt_e4m3_pitch(K), api.lpdt_e4m3_scale_pitch(K), -(-K // 128)
+    f, values = [], []
+    for rows in (M, N):
+        v = torch.randint(0, 9, (nodes, rows, K), generator=g, device="cuda")
+        e = torch.randint(0, 2, (nodes, rows, nb), generator=g, device="cuda")
+        q, s = (torch.full((nodes, rows, w), 0xA5, dtype=torch.uint8, device="cuda") for w in (P, S))
+        q[..., :K], s[..., :nb] = codes[v], (e + 127).to(torch.uint8)
+        f += [q, s]
+        values.append((v - 4).double() * torch.exp2(e.double()).repeat_interleave(128, -1)[..., :K])
+    want = torch.matmul(values[0], values[1].transpose(1, 2))
+    x = torch.randint(-99, 100, (nodes, M, N), generator=g, device="cuda").to(dtype) if addend else None
+    want = (want if x is None else want + x.double()).float().to(dtype)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for onto in ((x.clone(), torch.empty_like(x)) if addend else (torch.empty(nodes, M, N, dtype=dtype, device="cuda"),)):
+        api.lpdt_matmul_e4m3(nodes, M, N, K, *f, onto, addend=onto if addend and torch.equal(onto, x) else x, dev_status=status)
+        assert api.lpdt_last_kernel() == "lpdt::tc::matmul_e4m3_kernel" + form
+        assert torch.equal(onto, want)
+    assert api.lpdt_check_status(status) == 0
+
+
 @pytest.mark.parametrize("shape", [(2, 37, 100, 256), (1, 300, 515, 640), (3, 1, 64, 2048)])
 def test_matmul_into_a_flat_vector_and_onto_itself(shape):
     """Rows apart from one another inside a flat vector: nothing between them is written; addend = C accumulates."""
