@@ -21,18 +21,11 @@ __device__ __forceinline__ void rows_cluster_sync() {
 }
 __device__ __forceinline__ void rows_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void rows_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// To and from the same place of shared memory in the CTA of that rank.
+// To the same place of shared memory in the CTA of that rank.
 __device__ __forceinline__ void st_peer_u64(void *local, uint32_t rank, unsigned long long v) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
-}
-__device__ __forceinline__ unsigned long long ld_peer_u64(const void *local, uint32_t rank) {
-    uint32_t a;
-    unsigned long long v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
-    return v;
 }
 
 template <typename T>
@@ -85,12 +78,6 @@ __device__ __forceinline__ float vec_max_of(const uint4 &v, __half) {
     return fmaxf(__low2float(m), __high2float(m));
 }
 template <typename T> __device__ __forceinline__ float vec_max(const uint4 &v) { return vec_max_of(v, T()); }
-// A word of one value throughout.
-__device__ __forceinline__ uint4 same_word(float f) { const uint32_t b = __float_as_uint(f); return make_uint4(b, b, b, b); }
-template <typename H> __device__ __forceinline__ uint4 same_word(H h) {
-    const uint32_t s = *reinterpret_cast<const unsigned short *>(&h), b = s | (s << 16);
-    return make_uint4(b, b, b, b);
-}
 
 // Running sums relative to the maximum so far: s = sum 2^t, w = sum 2^t * t with t = (x - m) * c, c = log2(e) / temperature.
 // A value that is -inf, or far below m, counts as t = -10000 where w is taken: 2^t = 0 and no 0 * inf.  NaN passes through max_nan and
@@ -105,14 +92,6 @@ struct Stats {
         w = r * (w + t * s);
         s *= r;
         m = to;
-    }
-    __device__ __forceinline__ void join(const Stats &o, float c) {
-        Stats b = o;
-        const float to = fmaxf(m, b.m);
-        raise(to, c);
-        b.raise(to, c);
-        s += b.s;
-        w += b.w;
     }
 };
 // The largest of the lanes' numbers.
