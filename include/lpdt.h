@@ -305,7 +305,8 @@ lpdt_status lpdt_qconv_bwd_weight_affine(const lpdt_conv_desc *d, const uint8_t 
  *            x's columns.  Either pair may be NULL, not both.  A contraction over columns takes the first form, one over
  *            rows the second, so the three products of a linear layer Y = X W^T are lpdt_matmul_e4m3 of
  *            (X, W), (dY, W transposed) and (dY transposed, X transposed).
- * scale and scale_t need no alignment here.  Codes are written up to their pitch (zeros behind the last column).
+ * scale and scale_t need no alignment here.  Codes are written up to their pitch: zeros behind the last column, or 0x7f
+ * like the rest of the last block where that reads as NaN.  Scales behind the last block are not written.
  * Errors: INVALID_ARG, UNSUPPORTED (a dimension above 2^30, 2^31 blocks or more; the transposed form also above 65535 nodes
  * or 65535 * 128 rows), CUDA.  Empty matrices are a no-op.
  */

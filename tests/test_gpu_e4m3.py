@@ -88,6 +88,26 @@ def test_quantize_strided(dtype, offset, row_stride, node_stride):
         check_quantized(x, quantize(x, x_row_stride=row_stride, x_node_stride=node_stride, **kw))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("r,c", [(5, 131), (131, 5), (1, 1), (257, 300)])
+def test_quantize_behind_the_last_column(r, c, dtype):
+    """Codes up to the pitch are zeros, or NaN where the last block is; no scale behind the last block is written, and no byte behind the form."""
+    x = torch.randn(1, r, c, generator=torch.Generator().manual_seed(r)).to(dtype)
+    x[0, r - 1, c - 1] = float("nan")
+    x[0, 0, 0] = float("inf")
+    cols, rows = api.lpdt_e4m3_pitch(c), api.lpdt_e4m3_pitch(r)
+    for both in (False, True):
+        q, s = (torch.full((r + 1, w), 0xA5, dtype=torch.uint8, device="cuda") for w in (cols, api.lpdt_e4m3_scale_pitch(c)))
+        qt, st = (torch.full((c + 1, w), 0xA5, dtype=torch.uint8, device="cuda") for w in (rows, api.lpdt_e4m3_scale_pitch(r)))
+        api.lpdt_quantize_e4m3(x.cuda(), 1, r, c, q, s, qt if both else None, st if both else None)
+        for form, scales, size, length, values in ((q, s, r, c, x[0]), (qt, st, c, r, x[0].t()))[:1 + both]:
+            form, scales, blocks = form.cpu(), scales.cpu(), -(-length // 128)
+            bad = ~torch.isfinite(values[:, (blocks - 1) * 128:].float()).all(1)
+            assert (form[:size, length:] == torch.where(bad, 0x7f, 0).to(torch.uint8)[:, None]).all()
+            assert (scales[:size, blocks:] == 0xA5).all() and (scales[:size, blocks - 1] == 255).equal(bad)
+            assert (form[size:] == 0xA5).all() and (scales[size:] == 0xA5).all()
+
+
 def operands(nodes, M, N, K, seed, exact):
     """Codes and scales of A and B.  exact: small whole numbers, whose sums are whole numbers below 2^24."""
     rng = np.random.default_rng(seed)
