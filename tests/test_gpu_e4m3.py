@@ -194,6 +194,27 @@ def test_matmul_in_wide_tiles(shape, dtype):
     test_matmul(shape, dtype)
 
 
+@pytest.mark.parametrize("shape", [(1, 96, 160, 8192), (1, 1, 200, 16000), (1, 300, 300, 1000)])
+def test_matmul_loses_no_more_than_its_steps_cut(shape):
+    """A step adds 32 products to the sum, 33 values each cut below 2^-24 of the largest magnitude M among them and what is summed so far:
+    a bound for each element from its own partial sums, not from sum |a b|.  On the whole, cuts of products have either sign
+    and 1/sqrt(3) of their bound, those of the sum one: sqrt(steps * 32 / 3) + steps / 2 cuts, partial sums on average 2/3 of the last."""
+    nodes, M, N, K = shape
+    ops = operands(*shape, seed=K, exact=False)
+    C = torch.empty(nodes, M, N, device="cuda")
+    api.lpdt_matmul_e4m3(nodes, M, N, K, *device_operands(ops, K), C)
+    a, b = (torch.from_numpy(heads.dequantize_e4m3(ops[i], ops[i + 1])[0]).cuda() for i in (0, 2))
+    total, tol, steps = torch.zeros(M, N, dtype=torch.float64, device="cuda"), 0.0, -(-K // 32)
+    for k in range(0, K, 32):
+        largest = (a[:, k:k + 32].abs()[:, None] * b[:, k:k + 32].abs()[None]).amax(-1)
+        before = total.abs()
+        total = total + a[:, k:k + 32] @ b[:, k:k + 32].t()
+        tol = tol + 33 * 2.0 ** -24 * torch.maximum(torch.maximum(before, total.abs()), largest)
+    err = (C[0].double() - total).abs()
+    assert (err <= tol).all()
+    assert err.norm() <= ((steps * 32 / 3) ** 0.5 + steps / 2) * 2.0 ** -24 * total.norm()
+
+
 # The forms that a product takes, each with the kernel that has to answer: tiles of one turn and of several, K above and up to 8 blocks (from
 # where on the epilogue asks for the addend early), results of 4 and 2 bytes.
 F32, BF16, F16 = DTYPES
