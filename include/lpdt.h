@@ -661,8 +661,9 @@ lpdt_status lpdt_softmax_ce(int32_t nodes, int32_t B, int32_t K, const float *lo
  *   dlogits[r][v] = (1[v = tokens[r]] * g - p * (g + h * (ln p + entropy) - l)) / temperature
  * with g = d_logprob[r] (0 where the row has no token), h = d_entropy[r], l = d_lse[r]; each of the three nullable, not
  * all.  tokens is needed with d_logprob, entropy with d_entropy.  p is taken from the fp32 lse, so it is off by up to
- * 2^-23 * |lse| relative.  A row of nothing but mask values (lse < -1e30) has no gradient.  dlogits : `dtype`; it may be
- * the logits themselves with the same stride. */
+ * 2^-23 (|lse| + 2 |ln p|) relative, much of it one factor for the whole row: logits far from 0 lose digits here that the
+ * forward does not.  A row whose lse no fp32 holds (lse = +inf as written) answers NaN.  A row of nothing but mask values
+ * (lse < -1e30) has no gradient.  dlogits : `dtype`; it may be the logits themselves with the same stride. */
 lpdt_status lpdt_token_logprobs(int64_t rows, int32_t V, const void *logits, lpdt_dtype dtype, int64_t row_stride,
                                 float temperature, const int32_t *tokens, float *logprob, float *entropy, float *lse,
                                 int32_t top_k, float *top_logprob, int32_t *top_index, int32_t *dev_status, void *stream);

@@ -472,7 +472,8 @@ __global__ void __launch_bounds__(256) logprobs_bwd_kernel(const LogprobBwdArgs 
     const bool some = t >= 0 && t < a.V;
     const float lse = a.lse[row], g = a.g_logprob && some ? a.g_logprob[row] : 0.f;
     const float h = a.g_entropy ? a.g_entropy[row] : 0.f, l = a.g_lse ? a.g_lse[row] : 0.f;
-    const float base = l - g - (a.g_entropy ? h * a.entropy[row] : 0.f);
+    // (0 * lse: an lse beyond fp32 says nothing about p, so NaN and not the gradient of p = 0)
+    const float base = fmaf(0.f, lse, l - g - (a.g_entropy ? h * a.entropy[row] : 0.f));
     const bool none = lse < -1e30f;              // nothing but mask values: no gradient
     auto grad = [&](float x, int index) {
         const float lp = max_nan(fmaf(x, a.inv_t, -lse), kFar), p = ex2(lp * kLog2e);

@@ -243,6 +243,47 @@ def test_logprobs_backward(rows, V, temperature, which, dtype):
     within(d, want, tol + torch.finfo(dtype).eps / 2 * np.abs(want) + 2.0 ** -25)
 
 
+@pytest.mark.parametrize("V", [5, 3001])
+def test_logprobs_backward_of_logits_beyond_fp32(V):
+    """Logits / temperature whose lse no fp32 holds: the forward's log probabilities are right, lse is infinite, and the gradient, which has
+    nothing else to go by, is NaN and not that of probabilities 0.  Rows that stay in range beside them are as ever."""
+    x = logits_of(4, V, torch.float32, V)
+    x[1] = (x[1] * 4).round() * 1024 + 1e10
+    x[2] = -1e-29
+    x[2, 3] = 2e-30
+    tokens, T = np.array([0, 1, 3, 2]), 1e-30
+    x[0], x[3] = x[0] * 1e-30, x[3] * 1e-30
+    o, _ = report(x.cuda(), tokens, 0, T)
+    ref = heads.token_logprobs(x.double().numpy(), tokens, f32(T))
+    within(o["logprob"], ref["logprob"], SUM(V) + 2 * U * np.abs(ref["logprob"]))
+    d = torch.empty(4, V, device="cuda")
+    api.lpdt_token_logprobs_bwd(4, V, x.cuda(), torch.from_numpy(tokens.astype(np.int32)).cuda(), o["lse"], o["entropy"], d,
+                                d_logprob=torch.full((4,), 1e-30, device="cuda"), temperature=T)
+    assert torch.isinf(o["lse"][1]) and torch.isnan(d[1]).all()
+    want = heads.token_logprobs_bwd(x.double().numpy(), tokens, np.full(4, np.float32(1e-30), np.float64), temperature=f32(T))
+    keep = [0, 2, 3]
+    z = x.double().numpy()[keep] / f32(T)
+    within(d[keep], want[keep], (2 * np.abs(z).max() + SUM(V) / U + 16) * 2 * U)
+
+
+@pytest.mark.parametrize("V", [100, 3001])
+@pytest.mark.parametrize("shift", [0.0, 100.0, -1e4, 3e4])
+def test_logprobs_backward_of_shifted_rows(V, shift):
+    """The forward of shifted logits loses nothing but the rounding of the logits themselves; the gradient loses what the header says of
+    the fp32 lse, 2^-23 (|lse| + 2 |ln p|) of p, beside the sums' own rounding."""
+    x = (logits_of(3, V, torch.float32, V) * 64).round() / 64 + shift              # exact
+    tokens, g = np.arange(3), np.array([1.0, -2.0, 0.5], np.float32)
+    o, want = check_report(x, tokens, 0, 1.0)
+    base, _ = report((x - shift).cuda(), tokens)
+    within(o["logprob"], base["logprob"].double().cpu().numpy(), 2 * SUM(V) + 4 * U * np.abs(want["logprob"]))
+    d = torch.empty(3, V, device="cuda")
+    api.lpdt_token_logprobs_bwd(3, V, x.cuda(), torch.arange(3, dtype=torch.int32, device="cuda"), o["lse"], o["entropy"], d, d_logprob=torch.from_numpy(g).cuda())
+    ref = heads.token_logprobs_bwd(x.double().numpy(), tokens, g)
+    lp = x.double().numpy() - want["lse"][:, None]
+    off = 2 * U * (np.abs(want["lse"])[:, None] + 2 * np.abs(lp)) + SUM(V) + 8 * U
+    within(d, ref, np.abs(g)[:, None] * (np.exp(lp) * off + 2 * U))
+
+
 def test_logprobs_gradient_against_differences():
     """Central differences of the forward call itself: step 2^-4 of the logits; third derivatives are below 1, so the differences are
     off by at most step^2 / 6, and by the rounding of the forward over the step."""
