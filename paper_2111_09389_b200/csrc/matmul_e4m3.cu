@@ -15,11 +15,14 @@
 //
 // Two accumulators of up to 224 columns (the epilogue of one tile runs under the products of the next) and four sets of scale factors
 // fill the 512 columns of tensor memory; CTAs of one tile have one accumulator, and two of them fit an SM.  WIDE (G = 2): one accumulator of
-// up to 416 columns, made by two instructions that share the codes of the columns of C; a quarter less comes from L2 for the same
-// products.  Its epilogue is alone, but the next tile's loads go on under it, and they are the bound.
+// up to 416 columns, made by two instructions that share the codes of the columns of C: a quarter fewer bytes of codes for the same
+// products (18 % fewer read from L2 with the scales and what does not fill a tile).  Its epilogue is alone, but the next tile's loads go on
+// under it.
 //
-// Bound by the way from L2 to the SMs (some 40 bytes a cycle for pairs) and by power where that is long: 8192^3 with a bf16 result 404 us
-// (2722 TFLOP/s; 470 on two accumulators), 4096^3 58; one token x 4096 x 4096 7.5, launch and first loads being most of it.
+// Bound by the way from L2 to the SMs on two accumulators (48 bytes a cycle and SM, products 70 % of the cycles), by products (88 %) and the
+// clock under the power cap on wide tiles.  8192^3 with a bf16 result 404 us after a pause (2722 TFLOP/s; 470 on two accumulators); seconds
+// in a row at 1.34 to 1.41 GHz bf16 472 us (512 on two accumulators), fp32 485 (529), fp32 with an addend 532 (563).  4096^3 58; one token x
+// 4096 x 4096 7.5, launch and first loads being most of it.
 //
 // Roles per CTA: warp 0 fetches codes (TMA), warp 1 copies scale factors to tensor memory and issues the products, warp 2 brings the
 // scale bytes into the layout they are copied from, warps 4-11 run the epilogue.  Every wait on a barrier is bounded.
@@ -391,8 +394,10 @@ matmul_e4m3_kernel(const __grid_constant__ CUtensorMap mapL /*B: lanes*/, const 
         const int q = warp & 3, half = (warp - 4) >> 2, chunks = p.bn / 16;
         const uint32_t empty0 = G == 2 ? mm_peer(smem_u32(&ctl->tmem_empty[0]), 0) : smem_u32(&ctl->tmem_empty[0]);
         uint32_t tcount = 0;
-        // This warp's part of the accumulator is in registers.  The loads are complete, and nothing else is handed over; a release would
-        // wait for the stores to C of the whole tile (pairs: 8192 x 8192 x 512 77 us with it).
+        // This warp's part of the accumulator is in registers.  Relaxed is enough between CTAs: what is handed over is tensor memory alone,
+        // every lane's reads of it are complete (the wait for the loads), and they are ordered before the products that follow by the
+        // tcgen05 fences on both sides of the arrival, not by the arrival.  A release orders memory, of which the receiver reads none, and would
+        // wait for the stores to C of the whole tile (pairs: 8192 x 8192 x 512 77 us with it, 50 without).
         auto done = [&](int acc) {
             tc_fence_before();
             __syncwarp();

@@ -149,8 +149,9 @@ __global__ void __launch_bounds__(256) quantize_e4m3_rows_kernel(const E4m3Args 
 
 // A tile of 128 x 128 values, both forms (or the transposed one alone).  A warp holds R rows, a lane four columns of them as they
 // came: the R codes that a lane has of a column are R neighbouring bytes of the transposed form, turned through shared memory so that
-// they leave in rows of 128 bytes.  R = 16 rows of 16-bit elements or 8 of fp32 are 32 registers, which leaves room for as many CTAs as
-// keep memory busy while others compute.
+// they leave in rows of 128 bytes.  R = 16 rows of 16-bit elements or 8 of fp32 are 32 registers of the 64 that four CTAs an SM leave a
+// thread; the rest does not quite fit (spilled: bf16 and fp32 24 bytes, fp16 100; unaligned bf16 128, fp16 276, fp32 36), yet three or
+// five CTAs are no faster.
 template <typename T> struct TileShape {
     static constexpr int R = 32 / (int)sizeof(T), THREADS = kBlk / R * 32, MIN_CTAS = 1024 / THREADS;
 };
